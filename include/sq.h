@@ -60,7 +60,7 @@
 extern "C" {
 #endif
 
-#define SQ_ABI_VERSION 8
+#define SQ_ABI_VERSION 9
 
 typedef struct sq_store sq_store; /* opaque, library-owned host metadata */
 typedef int32_t sq_seq;           /* sequence handle: main thread or aux branch */
@@ -184,6 +184,8 @@ typedef struct {
   int64_t decode_kv_bytes_logical; /* same with every query's own tokens counted */
   int64_t extend_calls, extend_tokens; /* sq_extend_attn calls; query tokens they served */
   int64_t extend_kv_bytes;    /* K/V bytes of the keys those calls attended, each key once */
+  int64_t draft_calls, draft_tokens; /* sq_draft_attn calls; nodes they served */
+  int64_t draft_kv_bytes;     /* K/V bytes of the keys those calls read, each key once */
 } sq_stats;
 
 typedef struct {
@@ -220,6 +222,8 @@ typedef struct {
   int64_t evict_scan_launches, evict_gather_launches, append_launches;
   double extend_ms;
   int64_t extend_launches;
+  double qkv_ms, draft_ms; /* sq_qkv_store; sq_draft_attn with its merge */
+  int64_t qkv_launches, draft_launches;
 } sq_profile;
 
 /* ---- store -------------------------------------------------------------
@@ -458,14 +462,20 @@ sq_status sq_extend_attn(sq_store *store, int32_t layer, sq_seq seq, int32_t n_n
  *           to the keys at indices t - W + 1 .. t (the W most recent ones,
  *           its own included).  A decode query of a sequence of L tokens
  *           is at index L - 1; extend token j at L - n_new + j.
- *   reserved  must be 0.
+ *   first   F > 0: a windowed query also attends to the keys at indices 0 ..
+ *           F - 1 (the sequence's first tokens stay visible however far the
+ *           window has moved on; a key both name counts once).  Without a
+ *           window every key is visible and F changes nothing.
+ *   reserved, reserved2  must be 0.
  * The window is over logical indices of the (compacted) cache, as the
- * causal mask is.  SQ_ERR_INVALID: window < 0, reserved != 0, or a sinks
- * pointer that is not 4-byte aligned. */
+ * causal mask is.  SQ_ERR_INVALID: window < 0, first < 0, a reserved field
+ * that is not 0, or a sinks pointer that is not 4-byte aligned. */
 typedef struct sq_attn_opts {
   const float *sinks;
   int32_t window;
   int32_t reserved;
+  int32_t first;
+  int32_t reserved2;
 } sq_attn_opts;
 
 /* sq_decode_attn with options; opts NULL = sq_decode_attn.  A windowed
@@ -487,12 +497,149 @@ sq_status sq_extend_attn_ex(sq_store *store, int32_t layer, sq_seq seq, int32_t 
 sq_status sq_step_begin_ex(sq_store *store, const sq_seq *seqs, int32_t batch, int32_t mode,
                            int32_t window, void *stream);
 
+/* sq_step_begin_ex for a step whose windowed layers also see the first
+ * opts->first keys (opts->window and opts->first are used; opts->sinks is
+ * each layer's own).  opts NULL = sq_step_begin. */
+sq_status sq_step_begin_opts(sq_store *store, const sq_seq *seqs, int32_t batch, int32_t mode,
+                             const sq_attn_opts *opts, void *stream);
+
 /* sq_step_attn with options; opts NULL = sq_step_attn.  opts->window is 0
- * (every key) or the window of sq_step_begin_ex.  A capture replays with
- * the same options, each step begun with the same window.
- * SQ_ERR_INVALID also for any other window. */
+ * (every key) or the window of the step's begin, with its opts->first.  A
+ * capture replays with the same options, each step begun with the same
+ * window and first tokens.  SQ_ERR_INVALID also for any other window, or
+ * another opts->first with it. */
 sq_status sq_step_attn_ex(sq_store *store, int32_t layer, const void *k_new, const void *v_new,
                           const void *q, float *out, float scale, const sq_attn_opts *opts,
+                          void *stream);
+
+/* ---- tokens whose K and V come layer by layer ---------------------------
+ * A layered model knows layer l's keys and values only after layer l - 1 has
+ * attended.  sq_reserve appends the slots of a chunk of tokens at once
+ * (lengths, pages, positions, as sq_append would); sq_qkv_store then takes
+ * one layer's projections of those tokens and puts K and V into the slots,
+ * after which that layer's sq_extend_attn may run. */
+
+/* Norm of each query and key head and position rotation, in one pass.  For a
+ * head x of D channels at position p:
+ *   y = x * weight / sqrt(mean(x^2) + eps)          (weight NULL: y = x)
+ *   (a, b) -> (a cos - b sin, b cos + a sin) * mscale
+ * over the first rot_dim channels of y in pairs (i, i + rot_dim / 2), or
+ * (2 i, 2 i + 1) if interleaved, cos and sin of p * inv_freq[i] (the angle in
+ * 64 bits, everything else in fp32, rounded once).  inv_freq NULL: no
+ * rotation (rot_dim, interleaved and mscale are not used).
+ * SQ_ERR_INVALID: rot_dim not a multiple of 8 in [8, D]; eps negative or
+ * mscale not finite; a pointer that is not 4-byte aligned; interleaved other
+ * than 0 or 1. */
+typedef struct sq_qk_opts {
+  const float *inv_freq; /* device fp32 [rot_dim / 2], or NULL */
+  const float *q_weight; /* device fp32 [D], or NULL */
+  const float *k_weight; /* device fp32 [D], or NULL */
+  float eps;
+  float mscale;
+  int32_t rot_dim;
+  int32_t interleaved;
+} sq_qk_opts;
+
+/* The norm and rotation alone, for tokens anywhere (a decode step's, before
+ * sq_step_attn): q, k device bf16, token t's heads [heads][D] at q + t *
+ * q_stride and k + t * k_stride (elements, multiples of 8, at least heads *
+ * D; rows of a fused projection can be passed as they lie); positions device
+ * int32 [n], >= 0; q_out bf16 [n][num_q_heads][D], k_out bf16
+ * [n][num_kv_heads][D], packed, which may be q and k themselves where those
+ * are packed.  opts NULL: a copy.  Needs no store; work is enqueued on
+ * stream.  n = 0 does nothing.  SQ_ERR_INVALID: n < 0, head counts < 1, D
+ * other than 64 or 128, q, k, q_out or k_out null or not 16-byte aligned,
+ * positions null or not 4-byte aligned, a bad stride or option. */
+sq_status sq_qk_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                     const int32_t *positions, int32_t n, int32_t num_q_heads,
+                     int32_t num_kv_heads, int32_t head_dim, const sq_qk_opts *opts, void *q_out,
+                     void *k_out, void *stream);
+
+/* Append counts[b] tokens' slots to each of `batch` distinct sequences: pages
+ * in batch order, positions as sq_append.  Until the next call that changes a
+ * sequence of the store the tokens are open: sq_qkv_store takes their K and V
+ * layer by layer.  A slot whose layer has not been stored holds stale values.
+ * sq_reserve errors change nothing.  SQ_ERR_INVALID: batch outside [1,
+ * SQ_MAX_BATCH], a repeated sequence, a count < 1, more than SQ_MAX_RESERVE
+ * tokens, a sequence past its page-list capacity, positions past int32, an
+ * open draft; SQ_ERR_NO_PAGES.  A metadata-only store changes its metadata. */
+#define SQ_MAX_RESERVE 262144
+sq_status sq_reserve(sq_store *store, const sq_seq *seqs, const int32_t *counts, int32_t batch,
+                     void *stream);
+
+/* One layer's projections of the open tokens (sq_reserve's or
+ * sq_draft_begin's, in batch order; n of them in all): q normed and rotated to
+ * q_out (device bf16 [n][Hq][D], packed), k normed and rotated to the tokens'
+ * K slots, v to their V slots, in the store's precision (an 8-bit store takes
+ * k's code from the fp32 value).  q, k, v: device bf16, token t's heads at
+ * q + t * q_stride (elements) and so on, as for sq_qk_rope.  opts NULL: q and
+ * k as they are.  May be called for the layers in any order, and again.  Its
+ * launch depends on the arguments and the counts of the begin only: a capture
+ * replays for any later begin of the same counts.  SQ_ERR_INVALID: no open
+ * tokens, bad layer, pointers, strides or options, metadata-only store. */
+sq_status sq_qkv_store(sq_store *store, int32_t layer, const void *q, int64_t q_stride,
+                       const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                       const sq_qk_opts *opts, void *q_out, void *stream);
+
+/* Drop the tokens of seq from index `length` on (a rejected or abandoned
+ * tail): their pages lose a reference, and the next appended token gets the
+ * position of the first dropped one.  A last page that ends up part full
+ * while another branch holds it too is first copied to a new page.
+ * SQ_ERR_INVALID: length outside [0, length of seq], an open draft on seq;
+ * SQ_ERR_SPAN: a registered span ends past length; SQ_ERR_NO_PAGES: no page
+ * for that copy. */
+sq_status sq_truncate(sq_store *store, sq_seq seq, int64_t length, void *stream);
+
+/* ---- drafted tokens ------------------------------------------------------
+ * A draft proposes a tree of tokens for a sequence; the model runs all its
+ * nodes in one pass and keeps one path from a root.  sq_draft_begin gives
+ * every node a slot behind its sequence's tokens; per layer sq_qkv_store puts
+ * the nodes' K and V there and sq_draft_attn attends; sq_draft_accept keeps a
+ * path of each tree and drops the rest.
+ *
+ * While a draft is open its sequences take no other call than introspection
+ * (SQ_ERR_INVALID; accept empty paths to abandon it).  Other sequences do, but
+ * sq_reserve waits for its end.  Cached K and V must be finite, as for every
+ * attention call: a masked value counts with weight 0. */
+#define SQ_MAX_DRAFT 64 /* nodes of one sequence */
+
+/* Open a draft of counts[b] nodes for each of `batch` distinct sequences.
+ * parents: the nodes' parents, sequence after sequence; node i's is an earlier
+ * node of its sequence or -1 (a child of the sequence's last token; there may
+ * be several).  A node's depth counts its ancestors; its position is the
+ * sequence's next position + depth.  opts: window and first of the layers that
+ * will be windowed (NULL or window 0: none).
+ * SQ_ERR_INVALID: batch outside [1, SQ_MAX_BATCH], a repeated sequence, a
+ * count outside [1, SQ_MAX_DRAFT], a bad parent, an open draft, a sequence
+ * past its page-list capacity, a window over masked slots, more than 4096
+ * (sequence, KV head) rows of work, bad options; SQ_ERR_NO_PAGES.  Errors
+ * change nothing. */
+sq_status sq_draft_begin(sq_store *store, const sq_seq *seqs, const int32_t *counts, int32_t batch,
+                         const int32_t *parents, const sq_attn_opts *opts, void *stream);
+
+/* One layer's attention of the open draft's nodes.  q: device bf16
+ * [nodes][Hq][D], sequence after sequence; out: device fp32 alike; both
+ * 16-byte aligned.  Node i of a sequence of L tokens:
+ *   out[i][h] = sum_t softmax_t(scale * q[i][h] . K[t][h/G]) * V[t][h/G]
+ * over the sequence's L tokens, the node's ancestors and itself.  A window
+ * counts along the node's own path, on which a node of depth j has index L +
+ * j: it sees the indices L + depth - W + 1 .. L + depth, and those below
+ * opts->first.  opts->window is 0 or that of the begin, with its first; sinks
+ * as in sq_attn_opts.  The launches depend on the arguments and the begin's
+ * counts only: a capture replays for any later begin of the same counts,
+ * window and first tokens.  SQ_ERR_INVALID: no open draft, bad layer, pointer
+ * or options, scale not finite and positive, metadata-only store. */
+sq_status sq_draft_attn(sq_store *store, int32_t layer, const void *q, float *out, float scale,
+                        const sq_attn_opts *opts, void *stream);
+
+/* Keep a path of each sequence's tree and end the draft.  counts[b] nodes of
+ * sequence b (0: none), in `nodes` sequence after sequence (node numbers within
+ * the sequence): the first is a root, each next one a child of the one before.
+ * Their K and V of every layer and their positions move to the slots right
+ * behind the sequence's tokens; the other nodes' pages are freed.
+ * SQ_ERR_INVALID: no open draft, a count outside [0, the begin's], nodes that
+ * are no such path (the draft stays open). */
+sq_status sq_draft_accept(sq_store *store, const int32_t *counts, const int32_t *nodes,
                           void *stream);
 
 /* Host-only description of the work sq_decode_attn would do for this batch. */
@@ -545,7 +692,8 @@ int32_t sq_abi_version(void);
 
 /* Host call trace (off by default).  While open, every state-changing or
  * compute call (store create/destroy, sequence create, appends, span marks,
- * forks, releases, evictions, compaction, decode, decode steps, extend)
+ * forks, releases, evictions, compaction, truncation, decode, decode steps,
+ * extend, open tokens, drafts)
  * writes one line: "sq <call>(<arguments>) host_us=<time> ok" or
  * "... error: <message>", the time being the call's host time (device work
  * is only enqueued).  path "-" traces to stderr, another path appends to

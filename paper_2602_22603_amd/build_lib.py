@@ -18,7 +18,8 @@ ROOT = os.path.dirname(PKG_DIR)
 CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(PKG_DIR, "libsq.so")
-SOURCES = ["store.cpp", "kv_kernels.hip", "decode_kernels.hip", "extend_kernels.hip"]
+SOURCES = ["store.cpp", "kv_kernels.hip", "decode_kernels.hip", "extend_kernels.hip",
+           "open_kernels.hip", "draft_kernels.hip"]
 ARCH = "gfx950"
 
 # Packed fp32 VALU instructions are kept out of every HIP object.
@@ -36,10 +37,10 @@ def _hipcc():
     return path
 
 
-# Per-source additions.  The extend kernels' softmax takes maxima of MFMA
+# Per-source additions.  The extend and draft kernels' softmax takes maxima of MFMA
 # results, which are finite or -inf by construction: with NaN operands not
 # honoured, each v_max_f32 needs no canonicalising copy of its inputs.
-SOURCE_FLAGS = {"extend_kernels.hip": ["-fno-honor-nans"]}
+SOURCE_FLAGS = {"extend_kernels.hip": ["-fno-honor-nans"], "draft_kernels.hip": ["-fno-honor-nans"]}
 
 
 def _compile(hipcc, src, obj):

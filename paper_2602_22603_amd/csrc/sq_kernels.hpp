@@ -4,6 +4,8 @@
 #pragma once
 
 #include "decode_args.hpp"
+#include "draft_args.hpp"
 #include "extend_args.hpp"
 #include "kv_args.hpp"
+#include "open_args.hpp"
 #include "sq_common.hpp"

@@ -121,7 +121,7 @@ constexpr uint64_t kAlign = 256;
 uint64_t align_up(uint64_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
 
 struct Layout {
-  uint64_t pt, mask, keep, dst, src, upload, part_m, part_l, part_acc, step, scales, total;
+  uint64_t pt, mask, keep, dst, src, upload, part_m, part_l, part_acc, step, scales, open, total;
   uint64_t upload_elems;
 };
 
@@ -148,6 +148,7 @@ Layout layout_of(const sq_store_config &c) {
   L.part_acc = take((uint64_t)sq::kMaxItems * sq::kRows * c.head_dim * 4);
   L.step = take(sizeof(sq::StepPlan));
   L.scales = take((uint64_t)c.num_layers * 4 * 4);
+  L.open = take(sizeof(sq::OpenBlob));
   L.total = off;
   return L;
 }
@@ -206,6 +207,7 @@ struct Seq {
   // s attended); empty while no slot is masked.
   std::vector<uint16_t> kmask;
   int64_t n_masked = 0;
+  bool draft = false; // the last tokens are the nodes of an open draft
 };
 
 bool slot_kept(const Seq &q, int64_t i, int P) {
@@ -253,7 +255,7 @@ void grow_kmask(Seq &q) {
 }
 
 enum ProfKind { kProfValu, kProfMfma, kProfMerge, kProfScan, kProfGather, kProfAppend, kProfExtend,
-                kProfKinds };
+                kProfQkv, kProfDraft, kProfKinds };
 
 struct ProfPair {
   hipEvent_t a, b;
@@ -360,6 +362,13 @@ struct sq_store {
   hipEvent_t step_ev[2] = {nullptr, nullptr};
   bool step_pending[2] = {false, false};
   int step_buf = 0;
+  // open tokens (sq_reserve, sq_draft_begin): the plan in the workspace, two
+  // pinned host copies used in turn as the step plan's are
+  sq::OpenBlob *open_dev = nullptr;
+  sq::OpenBlob *open_staging[2] = {nullptr, nullptr};
+  hipEvent_t open_ev[2] = {nullptr, nullptr};
+  bool open_pending[2] = {false, false};
+  int open_buf = 0;
   bool have_last_evict = false;
   int64_t last_evict_L = 0, last_evict_Lp = 0;
 
@@ -383,9 +392,26 @@ struct sq_store {
     bool launch[2] = {false, false}; // VALU, MFMA
     int32_t grid[2] = {0, 0};
     int32_t window = 0; // the windowed plan's window (0: no windowed plan)
+    int32_t first = 0;  // and its first tokens
     int64_t kv_bytes = 0, kv_bytes_logical = 0;
     int64_t kv_bytes_w = 0, kv_bytes_logical_w = 0;
   } step;
+
+  // The open tokens: a reserved chunk's stay open while gen is what
+  // sq_reserve left, a draft's until it is accepted.
+  struct Open {
+    enum Kind { kNone, kChunk, kDraft } kind = kNone;
+    uint64_t gen = 0;
+    std::vector<sq_seq> seqs;
+    std::vector<int32_t> n;       // tokens by entry
+    std::vector<int64_t> base;    // length in front of them
+    std::vector<int64_t> pos0;
+    std::vector<int32_t> parents; // a draft's, entry after entry
+    int32_t total = 0, n_units = 0;
+    int32_t window = 0, first = 0;
+    int32_t rows = 0, n_wg = 0;
+    int64_t kv_bytes[2] = {0, 0};
+  } open;
 
   // profiling
   bool prof_on = false;
@@ -486,6 +512,13 @@ sq_status check_stream_store(sq_store *s) {
 }
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+bool aligned4(const void *p) { return ((uintptr_t)p & 3u) == 0; }
+
+// The nodes of an open draft are not tokens yet.
+sq_status no_draft(const Seq &q, sq_seq h) {
+  if (q.draft) return fail(SQ_ERR_INVALID, "sequence %d has an open draft (accept it first)", h);
+  return SQ_OK;
+}
 
 // Upload host int32 data to the workspace through the pinned staging buffer,
 // in stream order.  The staging buffer is reused only after the copy that
@@ -562,13 +595,14 @@ template <class T> int64_t first_diff(const T *a, const T *b, int64_t n) {
 }
 
 // keep_last >= 0: each entry attends only to its last keep_last cached
-// tokens (a window), read on its own; < 0: every token.  max_rb: row blocks
+// tokens (a window) and to its first keep_first, read on its own; < 0: every
+// token.  max_rb: row blocks
 // of 16 query rows a tile may take (2 for a plain decode call on a bf16
 // store, whose wide tiles then run on the two-block kernel; 1 for the
 // fused step, whose launches are fixed per batch and mode, and for an
 // 8-bit store).
 sq_status build_plan(sq_store *s, const sq_seq *seqs, int32_t batch, int32_t mode, Plan *plan,
-                     int64_t keep_last = -1, int max_rb = 1) {
+                     int64_t keep_last = -1, int max_rb = 1, int64_t keep_first = 0) {
   const int64_t tok_bytes = (int64_t)s->cfg.num_kv_heads * s->cfg.head_dim * 2 * s->elem_bytes();
   if (s->kv8) max_rb = 1;
   const int max_mem = std::min(sq::kMaxMembers, max_rb * sq::kRows / s->G);
@@ -670,10 +704,15 @@ sq_status build_plan(sq_store *s, const sq_seq *seqs, int32_t batch, int32_t mod
       };
 
   if (keep_last >= 0) {
-    // windows: [lo, L) from page lo / P, masked below lo % P on that page
+    // windows: [lo, L) from page lo / P, masked below lo % P on that page, and
+    // the first tokens, a segment of their own where they end in front of it
     for (int b = 0; b < batch; ++b) {
-      const int64_t L = s->seqs[seqs[b]].length, lo = std::max<int64_t>(0, L - keep_last);
-      plan->kv_bytes_logical += (L - lo) * tok_bytes;
+      const int64_t L = s->seqs[seqs[b]].length;
+      int64_t lo = std::max<int64_t>(0, L - keep_last);
+      const int64_t early = std::min(keep_first, lo);
+      if (early >= lo) lo = 0;
+      else if (early > 0) add_seg(seqs[b], 0, early, single_mfma, {b});
+      plan->kv_bytes_logical += (L - lo + (lo > 0 ? early : 0)) * tok_bytes;
       const int64_t p0 = lo / s->P;
       if (L > lo) add_seg(seqs[b], (int32_t)p0, L - p0 * s->P, single_mfma, {b}, (int32_t)(lo - p0 * s->P));
     }
@@ -850,7 +889,7 @@ struct ExtendPlan {
 // 5484 after 40: 66 with two, 52 with five).  Two splits of 256 rows, one
 // round of the CUs, stay the better cut from a prefix of a third on (8/8 heads
 // of 64, 8-bit store, 4037 after 1833: 99 us, 115 with three of 128 rows).
-ExtendPlan plan_extend(const sq_store *s, int64_t n, int64_t L, int64_t window) {
+ExtendPlan plan_extend(const sq_store *s, int64_t n, int64_t L, int64_t window, int64_t first = 0) {
   struct Tile {
     int rows, per_cu;
     double us, us_alone; // 64 keys, the CU full and one workgroup on it
@@ -878,8 +917,8 @@ ExtendPlan plan_extend(const sq_store *s, int64_t n, int64_t L, int64_t window) 
     const int64_t rows = tiles[t].rows, tq = rows / s->G;
     const int64_t qb = (n + tq - 1) / tq;
     int64_t kb = (L + sq::kExtKeys - 1) / sq::kExtKeys; // the last query block's key blocks
-    if (window > 0) // a query block's keys span at most W + TQ - 1 indices
-      kb = std::min<int64_t>(kb, (window + tq - 2) / sq::kExtKeys + 2);
+    if (window > 0) // a query block's keys span at most W + TQ - 1 indices, and the first tokens
+      kb = std::min<int64_t>(kb, (window + tq - 2) / sq::kExtKeys + 2 + (first + sq::kExtKeys - 1) / sq::kExtKeys);
     // a query block sees this many key blocks fewer than the one after it
     const double fewer = window > 0 ? 0.0 : (double)tq / sq::kExtKeys;
     const int64_t wg = qb * hkv, slots = (int64_t)s->cus * tiles[t].per_cu;
@@ -1029,6 +1068,7 @@ sq_status sq_store_create(const sq_store_config *cfg, sq_store **out) {
     s->part_l = reinterpret_cast<float *>(ws + lay.part_l);
     s->part_acc = reinterpret_cast<float *>(ws + lay.part_acc);
     s->step_dev = reinterpret_cast<sq::StepPlan *>(ws + lay.step);
+    s->open_dev = reinterpret_cast<sq::OpenBlob *>(ws + lay.open);
     sq::Pools &p = s->pools;
     p.k = static_cast<uint16_t *>(cfg->k_pool);
     p.v = static_cast<uint16_t *>(cfg->v_pool);
@@ -1095,6 +1135,11 @@ sq_status sq_store_create(const sq_store_config *cfg, sq_store **out) {
         s->step_staging[i] = static_cast<sq::StepPlan *>(sh);
         e = hipEventCreateWithFlags(&s->step_ev[i], hipEventDisableTiming);
       }
+      if (e == hipSuccess) e = hipHostMalloc(&sh, sizeof(sq::OpenBlob), hipHostMallocDefault);
+      if (e == hipSuccess) {
+        s->open_staging[i] = static_cast<sq::OpenBlob *>(sh);
+        e = hipEventCreateWithFlags(&s->open_ev[i], hipEventDisableTiming);
+      }
     }
     if (e != hipSuccess) {
       (void)hipEventDestroy(s->staging_ev);
@@ -1102,9 +1147,11 @@ sq_status sq_store_create(const sq_store_config *cfg, sq_store **out) {
       for (int i = 0; i < 2; ++i) {
         if (s->step_staging[i]) (void)hipHostFree(s->step_staging[i]);
         if (s->step_ev[i]) (void)hipEventDestroy(s->step_ev[i]);
+        if (s->open_staging[i]) (void)hipHostFree(s->open_staging[i]);
+        if (s->open_ev[i]) (void)hipEventDestroy(s->open_ev[i]);
       }
       delete s;
-      return hip_fail(e, "step plan staging");
+      return hip_fail(e, "plan staging");
     }
   }
   *out = s;
@@ -1128,6 +1175,9 @@ sq_status sq_store_destroy(sq_store *s) {
       if (s->step_pending[i]) (void)hipEventSynchronize(s->step_ev[i]);
       if (s->step_ev[i]) (void)hipEventDestroy(s->step_ev[i]);
       if (s->step_staging[i]) (void)hipHostFree(s->step_staging[i]);
+      if (s->open_pending[i]) (void)hipEventSynchronize(s->open_ev[i]);
+      if (s->open_ev[i]) (void)hipEventDestroy(s->open_ev[i]);
+      if (s->open_staging[i]) (void)hipHostFree(s->open_staging[i]);
     }
   }
   delete s;
@@ -1156,6 +1206,7 @@ sq_status sq_append(sq_store *s, sq_seq h, int32_t n, const void *k_new, const v
   Seq *q = s->get(h);
   if (!q) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", h);
   if (n < 0) return fail(SQ_ERR_INVALID, "negative token count");
+  if (sq_status r = no_draft(*q, h)) return r;
   if (n == 0) return SQ_OK;
   const int64_t new_len = q->length + n;
   const int64_t want = (new_len + s->P - 1) / s->P;
@@ -1222,7 +1273,9 @@ sq_status take_opts(const sq_attn_opts *opts, sq_attn_opts *o) {
   *o = sq_attn_opts{};
   if (!opts) return SQ_OK;
   if (opts->window < 0) return fail(SQ_ERR_INVALID, "window %d < 0", opts->window);
-  if (opts->reserved != 0) return fail(SQ_ERR_INVALID, "sq_attn_opts.reserved must be 0");
+  if (opts->reserved != 0 || opts->reserved2 != 0)
+    return fail(SQ_ERR_INVALID, "sq_attn_opts.reserved and reserved2 must be 0");
+  if (opts->first < 0) return fail(SQ_ERR_INVALID, "first %d < 0", opts->first);
   if (((uintptr_t)opts->sinks & 3u) != 0) return fail(SQ_ERR_INVALID, "sinks must be 4-byte aligned");
   *o = *opts;
   return SQ_OK;
@@ -1237,6 +1290,7 @@ sq_status check_one_token_each(sq_store *s, const sq_seq *seqs, int32_t batch) {
     if (!q) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", seqs[b]);
     for (int c = 0; c < b; ++c)
       if (seqs[c] == seqs[b]) return fail(SQ_ERR_INVALID, "sequence %d repeated in the batch", seqs[b]);
+    if (sq_status r = no_draft(*q, seqs[b])) return r;
     if (q->length % s->P == 0) {
       if (q->length / s->P + 1 > s->cfg.max_pages_per_seq)
         return fail(SQ_ERR_INVALID, "sequence %d is at its page-list capacity", seqs[b]);
@@ -1293,10 +1347,13 @@ sq_status decode_call(sq_store *s, int32_t layer, const sq_seq *seqs, int32_t ba
   if (!q || !out || !aligned16(q) || !aligned16(out))
     return fail(SQ_ERR_INVALID, "q and out must be non-null and 16-byte aligned");
   if (!std::isfinite(scale)) return fail(SQ_ERR_INVALID, "scale must be finite");
-  for (int b = 0; b < batch; ++b)
-    if (!s->get(seqs[b])) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", seqs[b]);
+  for (int b = 0; b < batch; ++b) {
+    const Seq *sq = s->get(seqs[b]);
+    if (!sq) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", seqs[b]);
+    if ((r = no_draft(*sq, seqs[b]))) return r;
+  }
   Plan plan;
-  r = build_plan(s, seqs, batch, mode, &plan, o.window > 0 ? o.window : -1, 2);
+  r = build_plan(s, seqs, batch, mode, &plan, o.window > 0 ? o.window : -1, 2, o.first);
   if (r != SQ_OK) return r;
   if (plan.masked && o.window > 0)
     return fail(SQ_ERR_INVALID, "a window over a sequence with masked slots (compact it first)");
@@ -1378,6 +1435,7 @@ sq_status sq_span_mark(sq_store *s, sq_seq h, int32_t cursor, int64_t start, int
   if (!s) return fail(SQ_ERR_INVALID, "null store");
   Seq *q = s->get(h);
   if (!q) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", h);
+  if (sq_status r = no_draft(*q, h)) return r;
   if (cursor < 0 || q->spans.count(cursor))
     return fail(SQ_ERR_INVALID, "cursor %d negative or already registered", cursor);
   if (!(0 <= start && start <= end && end <= q->length))
@@ -1403,6 +1461,7 @@ sq_status sq_fork(sq_store *s, sq_seq parent, int64_t fork_len, sq_seq *child, v
   if (!s || !child) return fail(SQ_ERR_INVALID, "null argument");
   Seq *par = s->get(parent);
   if (!par) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", parent);
+  if (sq_status r = no_draft(*par, parent)) return r;
   if (!(0 <= fork_len && fork_len <= par->length))
     return fail(SQ_ERR_INVALID, "fork point %lld outside [0, %lld]", (long long)fork_len,
                 (long long)par->length);
@@ -1467,6 +1526,7 @@ sq_status sq_release(sq_store *s, sq_seq h) {
   if (!s) return fail(SQ_ERR_INVALID, "null store");
   Seq *q = s->get(h);
   if (!q) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", h);
+  if (sq_status r = no_draft(*q, h)) return r;
   ++s->gen;
   for (int32_t p : q->pages) s->unref(p, nullptr);
   *q = Seq();
@@ -1591,6 +1651,7 @@ sq_status sq_evict_spans_ex(sq_store *s, sq_seq h, const int32_t *cursor_ids, in
   Seq *q = s->get(h);
   if (!q) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", h);
   ++s->gen; // ends a begun decode step even when the call fails
+  if (sq_status r = no_draft(*q, h)) return r;
   if (n < 0 || n > SQ_MAX_EVICT_SPANS)
     return fail(SQ_ERR_INVALID, "cursor count %d outside [0, %d]", n, SQ_MAX_EVICT_SPANS);
   if (n > 0 && !cursor_ids) return fail(SQ_ERR_INVALID, "null cursor list");
@@ -1914,6 +1975,574 @@ sq_status sq_evict_spans_ex(sq_store *s, sq_seq h, const int32_t *cursor_ids, in
   return SQ_OK;
 }
 
+// ---- tokens whose K and V come layer by layer --------------------------------
+namespace {
+
+// The shape of a draft's work: query rows per workgroup and workgroups of a
+// launch.  They follow from the counts alone, so that a captured layer replays
+// for later drafts of the same counts.  A tile of 256 rows (eight waves, one
+// workgroup a CU), 128 or 64 (two a CU) is the smallest that holds the largest
+// tree's rows; more than 256 take two tiles.
+void draft_shape(const sq_store *s, int32_t most_nodes, int32_t *rows, int32_t *n_wg) {
+  const int r = most_nodes * s->G;
+  *rows = r <= 64 ? 64 : r <= 128 ? 128 : 256;
+  const int64_t wg = (int64_t)s->cus * (*rows == 256 ? 1 : 2);
+  // every workgroup may leave two partial slots of `rows` rows
+  *n_wg = (int32_t)std::min<int64_t>({wg, sq::kDraftWgs, (int64_t)sq::kMaxItems * sq::kRows / *rows / 2});
+}
+
+// Deals the rows' blocks (nb[t] for every KV head of tile t) out to at most n_wg
+// workgroups in equal runs; kRowStart blocks stand for the start of a row.
+constexpr int64_t kRowStart = 1;
+constexpr int64_t kMinRun = 3; // blocks a workgroup takes at least
+void draft_split(const std::vector<int64_t> &nb, int hkv, int32_t n_wg, sq::DraftSplit *out) {
+  int64_t total = 0;
+  for (int64_t b : nb) total += (b + kRowStart) * hkv;
+  const int64_t n = std::max<int64_t>(1, std::min<int64_t>(n_wg, total / kMinRun));
+  int32_t n_pieces = 0, slots = 0;
+  int64_t w = 0, at = 0; // the workgroup at flattened block `at`
+  auto end_of = [&](int64_t x) { return (x + 1) * total / n; };
+  out->piece0[0] = 0;
+  for (size_t t = 0; t < nb.size(); ++t)
+    for (int g = 0; g < hkv; ++g) {
+      const int32_t row = (int32_t)t * hkv + g, first = n_pieces;
+      int64_t b = 0;
+      const int64_t stop = at + nb[t] + kRowStart;
+      while (at < stop) {
+        while (end_of(w) <= at) out->piece0[++w] = n_pieces;
+        const int64_t upto = std::min(stop, end_of(w));
+        const int64_t e = std::min<int64_t>(nb[t], b + upto - at);
+        if (e > b) out->pieces[n_pieces++] = {row, (int32_t)b, (int32_t)e, -1};
+        b = e;
+        at = upto;
+      }
+      const int32_t cnt = n_pieces - first;
+      out->merge[row] = {slots, cnt > 1 ? cnt : 0};
+      if (cnt > 1)
+        for (int32_t i = first; i < n_pieces; ++i) out->pieces[i].slot = slots++;
+    }
+  while (w < n_wg) out->piece0[++w] = n_pieces;
+}
+
+// Depths of a tree's nodes; false for a parent that is no earlier node or -1.
+bool tree_depths(const int32_t *parents, int32_t n, int32_t *depth) {
+  for (int32_t i = 0; i < n; ++i) {
+    if (parents[i] < -1 || parents[i] >= i) return false;
+    depth[i] = parents[i] < 0 ? 0 : depth[parents[i]] + 1;
+  }
+  return true;
+}
+
+// sq_reserve (parents null) and sq_draft_begin.
+sq_status open_tokens(sq_store *s, const sq_seq *seqs, const int32_t *counts, int32_t batch,
+                      const int32_t *parents, const sq_attn_opts &o, void *stream) {
+  const bool draft = parents != nullptr;
+  if (batch < 1 || batch > SQ_MAX_BATCH) return fail(SQ_ERR_INVALID, "batch must be in [1, %d]", SQ_MAX_BATCH);
+  if (s->open.kind == sq_store::Open::kDraft) return fail(SQ_ERR_INVALID, "a draft is open (accept it first)");
+  int64_t need = 0, total = 0;
+  int32_t most = 0;
+  std::vector<int32_t> depth;
+  for (int b = 0; b < batch; ++b) {
+    const Seq *q = s->get(seqs[b]);
+    if (!q) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", seqs[b]);
+    for (int c = 0; c < b; ++c)
+      if (seqs[c] == seqs[b]) return fail(SQ_ERR_INVALID, "sequence %d repeated in the batch", seqs[b]);
+    const int64_t n = counts[b];
+    if (n < 1 || (draft && n > SQ_MAX_DRAFT) || total + n > SQ_MAX_RESERVE)
+      return fail(SQ_ERR_INVALID, "%lld tokens of sequence %d: at least 1, at most %d", (long long)n, seqs[b],
+                  draft ? SQ_MAX_DRAFT : SQ_MAX_RESERVE);
+    const int64_t want = (q->length + n + s->P - 1) / s->P;
+    if (want > s->cfg.max_pages_per_seq)
+      return fail(SQ_ERR_INVALID, "sequence %d would need %lld pages (max %d)", seqs[b], (long long)want,
+                  s->cfg.max_pages_per_seq);
+    if (s->device && q->next_pos + n > INT32_MAX) return fail(SQ_ERR_INVALID, "positions exceed int32");
+    if (draft) {
+      depth.resize(total + n);
+      if (!tree_depths(parents + total, (int32_t)n, depth.data() + total))
+        return fail(SQ_ERR_INVALID, "sequence %d: a node's parent must be an earlier node or -1", seqs[b]);
+      if (o.window > 0 && q->n_masked > 0)
+        return fail(SQ_ERR_INVALID, "a window over a sequence with masked slots (compact it first)");
+    }
+    need += want - (int64_t)q->pages.size();
+    most = std::max(most, (int32_t)n);
+    total += n;
+  }
+  if (need > s->n_free)
+    return fail(SQ_ERR_NO_PAGES, "%lld pages needed, %lld free", (long long)need, (long long)s->n_free);
+  int32_t rows = 0, n_wg = 0, per_tile = 0;
+  if (draft && s->device) {
+    draft_shape(s, most, &rows, &n_wg);
+    per_tile = rows / s->G;
+    int64_t n_rows = 0;
+    for (int b = 0; b < batch; ++b) n_rows += (int64_t)((counts[b] + per_tile - 1) / per_tile) * s->cfg.num_kv_heads;
+    if (n_rows > sq::kDraftRows)
+      return fail(SQ_ERR_INVALID, "the draft needs %lld (sequence, KV head) rows (max %d)", (long long)n_rows,
+                  sq::kDraftRows);
+  }
+  const int sb = s->open_buf;
+  if (s->device && s->open_pending[sb]) { // this staging copy's last upload
+    hipError_t e = hipEventSynchronize(s->open_ev[sb]);
+    if (e != hipSuccess) return hip_fail(e, "hipEventSynchronize(open tokens)");
+    s->open_pending[sb] = false;
+  }
+  sq::OpenBlob *bl = s->device ? s->open_staging[sb] : nullptr;
+
+  ++s->gen;
+  sq_store::Open &op = s->open;
+  op = sq_store::Open{};
+  op.kind = draft ? sq_store::Open::kDraft : sq_store::Open::kChunk;
+  op.gen = s->gen;
+  op.total = (int32_t)total;
+  op.rows = rows;
+  op.n_wg = n_wg;
+  op.window = o.window;
+  op.first = o.first;
+  if (draft) op.parents.assign(parents, parents + total);
+  sq::OpenArgs oa{};
+  oa.plan.batch = batch;
+  oa.plan.total = (int32_t)total;
+  std::vector<int64_t> nb[2];
+  int32_t tok0 = 0, n_tiles = 0;
+  const int64_t tok_bytes = (int64_t)s->cfg.num_kv_heads * s->cfg.head_dim * 2 * s->elem_bytes();
+  for (int b = 0; b < batch; ++b) {
+    Seq &q = s->seqs[seqs[b]];
+    const int64_t base = q.length, n = counts[b], want = (base + n + s->P - 1) / s->P;
+    op.seqs.push_back(seqs[b]);
+    op.n.push_back((int32_t)n);
+    op.base.push_back(base);
+    op.pos0.push_back(q.next_pos);
+    while ((int64_t)q.pages.size() < want) q.pages.push_back(s->alloc_page());
+    grow_kmask(q);
+    if (draft) {
+      const int64_t pos0 = q.next_pos;
+      for (int64_t i = 0; i < n; ++i) { // a run of positions per node at worst
+        q.next_pos = pos0 + depth[tok0 + i];
+        runs_append(q, 1);
+        ++q.length;
+      }
+      q.next_pos = pos0;
+      q.draft = true;
+    } else {
+      runs_append(q, n);
+      q.length += n;
+      q.next_pos += n;
+      s->st.append_tokens += n;
+    }
+    if (!s->device) {
+      tok0 += (int32_t)n;
+      continue;
+    }
+    oa.row[b] = seqs[b];
+    oa.pos0[b] = (int32_t)op.pos0[b];
+    oa.plan.base[b] = (int32_t)base;
+    oa.plan.n[b] = (int32_t)n;
+    oa.plan.tok0[b] = tok0;
+    oa.plan.unit0[b] = op.n_units;
+    const int32_t units = sq::open_units(n);
+    for (int32_t u = 0; u < units; ++u) {
+      const int64_t pg = base / s->P + u;
+      bl->ids[op.n_units + u] = pg < want ? q.pages[pg] : -1;
+    }
+    op.n_units += units;
+    if (draft) {
+      const int64_t L = base + n, blocks = (L + sq::kExtKeys - 1) / sq::kExtKeys;
+      for (int64_t i = 0; i < n; ++i) {
+        sq::DraftNode &nd = bl->nodes[tok0 + i];
+        const int32_t p = parents[tok0 + i], d = depth[tok0 + i];
+        nd.anc[0] = (p < 0 ? 0 : bl->nodes[tok0 + p].anc[0]) | 1ull << i;
+        nd.anc[1] = nd.anc[0];
+        nd.lo = 0;
+        if (o.window > 0) {
+          const int64_t lo = base + d - o.window + 1; // first index of the window
+          for (int64_t j = 0; j < i; ++j)
+            if (base + depth[tok0 + j] < lo && base + depth[tok0 + j] >= o.first) nd.anc[1] &= ~(1ull << j);
+          nd.lo = (int32_t)std::min(base, std::max<int64_t>(0, lo));
+        }
+        bl->depth[tok0 + i] = d;
+      }
+      int64_t lo_seq = L;
+      for (int32_t i0 = 0; i0 < n; i0 += per_tile, ++n_tiles) {
+        sq::DraftTile &t = bl->tiles[n_tiles];
+        t = sq::DraftTile{};
+        t.row = seqs[b];
+        t.base = (int32_t)base;
+        t.n = (int32_t)n;
+        t.n_pages = (int32_t)q.pages.size();
+        t.node0 = tok0 + i0;
+        t.n_nodes = std::min<int32_t>(per_tile, (int32_t)n - i0);
+        t.masked = q.n_masked > 0 ? 1 : 0;
+        int32_t lo_min = INT32_MAX;
+        for (int32_t i = 0; i < t.n_nodes; ++i) {
+          sq::DraftNode &nd = bl->nodes[t.node0 + i];
+          nd.tile = n_tiles;
+          lo_min = std::min(lo_min, nd.lo);
+          t.lo_max[1] = std::max(t.lo_max[1], nd.lo);
+        }
+        // windowed: the first tokens' blocks, then those from the window's start
+        const int32_t from = lo_min / sq::kExtKeys;
+        t.nf[1] = std::min<int32_t>((int32_t)(((int64_t)o.first + sq::kExtKeys - 1) / sq::kExtKeys), from);
+        t.skip[1] = from - t.nf[1];
+        nb[0].push_back(blocks);
+        nb[1].push_back(blocks - t.skip[1]);
+        lo_seq = std::min<int64_t>(lo_seq, lo_min);
+      }
+      op.kv_bytes[0] += L * tok_bytes;
+      op.kv_bytes[1] += (L - lo_seq + std::min<int64_t>(o.first, lo_seq)) * tok_bytes;
+    }
+    tok0 += (int32_t)n;
+  }
+  oa.plan.unit0[batch] = op.n_units;
+  oa.plan.n_units = op.n_units;
+  if (!s->device) return SQ_OK;
+
+  auto part = [&](const void *at, size_t bytes) {
+    const int32_t n16 = (int32_t)((bytes + 15) / 16);
+    oa.seg_off[oa.n_segs] = (int32_t)(static_cast<const char *>(at) - reinterpret_cast<const char *>(bl));
+    oa.seg_n16[oa.n_segs++] = n16;
+    oa.n16 += n16;
+  };
+  part(bl->ids, op.n_units * sizeof(int32_t));
+  if (draft) {
+    part(bl->tiles, n_tiles * sizeof(sq::DraftTile));
+    part(bl->nodes, total * sizeof(sq::DraftNode));
+    for (int w = 0; w < (o.window > 0 ? 2 : 1); ++w) {
+      sq::DraftSplit &sp = bl->split[w];
+      draft_split(nb[w], s->cfg.num_kv_heads, n_wg, &sp);
+      part(sp.merge, (size_t)n_tiles * s->cfg.num_kv_heads * sizeof(sq::DraftMerge));
+      part(sp.piece0, (n_wg + 1) * sizeof(int32_t));
+      part(sp.pieces, sp.piece0[n_wg] * sizeof(sq::DraftPiece));
+    }
+  }
+  oa.src = reinterpret_cast<const char *>(bl);
+  oa.dst = reinterpret_cast<char *>(s->open_dev);
+  oa.ids = bl->ids;
+  oa.depth = draft ? bl->depth : nullptr;
+  oa.pt = s->pt_dev;
+  oa.pos = s->pools.pos;
+  oa.max_pages = s->cfg.max_pages_per_seq;
+  hipStream_t strm = static_cast<hipStream_t>(stream);
+  s->last_stream = strm;
+  hipError_t e = sq::launch_open(oa, strm);
+  if (e != hipSuccess) return hip_fail(e, "open tokens");
+  e = hipEventRecord(s->open_ev[sb], strm);
+  if (e != hipSuccess) return hip_fail(e, "hipEventRecord(open tokens)");
+  s->open_pending[sb] = true;
+  s->open_buf = 1 - sb;
+  return SQ_OK;
+}
+
+// Norm and rotation options, checked; null = none.
+sq_status take_qk_opts(const sq_qk_opts *opts, int D, sq::QkArgs *a) {
+  a->mscale = 1.f;
+  if (!opts) return SQ_OK;
+  if (!aligned4(opts->inv_freq) || !aligned4(opts->q_weight) || !aligned4(opts->k_weight))
+    return fail(SQ_ERR_INVALID, "inv_freq, q_weight and k_weight must be 4-byte aligned");
+  if (!std::isfinite(opts->eps) || opts->eps < 0.f) return fail(SQ_ERR_INVALID, "eps must be finite and not negative");
+  if (opts->inv_freq) {
+    if (opts->rot_dim < 8 || opts->rot_dim > D || opts->rot_dim % 8)
+      return fail(SQ_ERR_INVALID, "rot_dim %d: a multiple of 8 in [8, %d]", opts->rot_dim, D);
+    if (opts->interleaved != 0 && opts->interleaved != 1) return fail(SQ_ERR_INVALID, "interleaved must be 0 or 1");
+    if (!std::isfinite(opts->mscale)) return fail(SQ_ERR_INVALID, "mscale must be finite");
+    a->inv_freq = opts->inv_freq;
+    a->rot = opts->rot_dim;
+    a->interleaved = opts->interleaved;
+    a->mscale = opts->mscale;
+  }
+  a->q_weight = opts->q_weight;
+  a->k_weight = opts->k_weight;
+  a->eps = opts->eps;
+  return SQ_OK;
+}
+
+// Rows of `heads` heads of D, `stride` elements apart.
+sq_status check_rows(const void *p, int64_t stride, int64_t heads, int D, const char *what) {
+  if (!p || !aligned16(p)) return fail(SQ_ERR_INVALID, "%s must be non-null and 16-byte aligned", what);
+  if (stride < heads * D || stride % 8)
+    return fail(SQ_ERR_INVALID, "%s: a row stride of %lld elements (a multiple of 8, at least %lld)", what,
+                (long long)stride, (long long)heads * D);
+  return SQ_OK;
+}
+
+bool capturing(hipStream_t strm) {
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  (void)hipStreamIsCapturing(strm, &cap);
+  return cap != hipStreamCaptureStatusNone;
+}
+
+// The open draft, if there is one.
+sq_status open_draft(sq_store *s) {
+  if (s->open.kind != sq_store::Open::kDraft) return fail(SQ_ERR_INVALID, "no draft is open");
+  return SQ_OK;
+}
+
+} // namespace
+
+sq_status sq_qk_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride,
+                     const int32_t *positions, int32_t n, int32_t num_q_heads,
+                     int32_t num_kv_heads, int32_t head_dim, const sq_qk_opts *opts, void *q_out,
+                     void *k_out, void *stream) {
+  SQ_TRACE_CALL("sq_qk_rope", "n=%d q_heads=%d kv_heads=%d head_dim=%d", n, num_q_heads, num_kv_heads, head_dim);
+  if (n < 0 || num_q_heads < 1 || num_kv_heads < 1) return fail(SQ_ERR_INVALID, "n must be >= 0, head counts >= 1");
+  if (head_dim != 64 && head_dim != 128) return fail(SQ_ERR_INVALID, "head_dim must be 64 or 128");
+  sq::QkArgs a{};
+  sq_status r = take_qk_opts(opts, head_dim, &a);
+  if (r != SQ_OK || n == 0) return r;
+  if ((r = check_rows(q, q_stride, num_q_heads, head_dim, "q"))) return r;
+  if ((r = check_rows(k, k_stride, num_kv_heads, head_dim, "k"))) return r;
+  if (!q_out || !k_out || !aligned16(q_out) || !aligned16(k_out))
+    return fail(SQ_ERR_INVALID, "q_out and k_out must be non-null and 16-byte aligned");
+  if (!positions || !aligned4(positions)) return fail(SQ_ERR_INVALID, "positions must be non-null and 4-byte aligned");
+  a.q = static_cast<const uint16_t *>(q);
+  a.k = static_cast<const uint16_t *>(k);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.q_out = static_cast<uint16_t *>(q_out);
+  a.k_out = static_cast<uint16_t *>(k_out);
+  a.pos = positions;
+  a.n = n;
+  a.hq = num_q_heads;
+  a.hkv = num_kv_heads;
+  hipError_t e = sq::launch_qk(head_dim, a, static_cast<hipStream_t>(stream));
+  return e == hipSuccess ? SQ_OK : hip_fail(e, "norm and rotation kernel");
+}
+
+sq_status sq_reserve(sq_store *s, const sq_seq *seqs, const int32_t *counts, int32_t batch, void *stream) {
+  SQ_TRACE_CALL("sq_reserve", "store=%p batch=%d", (void *)s, batch);
+  if (!s || !seqs || !counts) return fail(SQ_ERR_INVALID, "null argument");
+  return open_tokens(s, seqs, counts, batch, nullptr, sq_attn_opts{}, stream);
+}
+
+sq_status sq_draft_begin(sq_store *s, const sq_seq *seqs, const int32_t *counts, int32_t batch,
+                         const int32_t *parents, const sq_attn_opts *opts, void *stream) {
+  SQ_TRACE_CALL("sq_draft_begin", "store=%p batch=%d window=%d first=%d", (void *)s, batch, opts ? opts->window : 0, opts ? opts->first : 0);
+  if (!s || !seqs || !counts || !parents) return fail(SQ_ERR_INVALID, "null argument");
+  sq_attn_opts o{};
+  sq_status r = take_opts(opts, &o);
+  if (r != SQ_OK) return r;
+  return open_tokens(s, seqs, counts, batch, parents, o, stream);
+}
+
+sq_status sq_qkv_store(sq_store *s, int32_t layer, const void *q, int64_t q_stride, const void *k,
+                       int64_t k_stride, const void *v, int64_t v_stride, const sq_qk_opts *opts,
+                       void *q_out, void *stream) {
+  SQ_TRACE_CALL("sq_qkv_store", "store=%p layer=%d tokens=%d", (void *)s, layer, s ? s->open.total : 0);
+  if (!s) return fail(SQ_ERR_INVALID, "null store");
+  if (!s->device) return fail(SQ_ERR_INVALID, "metadata-only store holds no K and V");
+  const sq_store::Open &op = s->open;
+  if (op.kind == sq_store::Open::kNone || (op.kind == sq_store::Open::kChunk && op.gen != s->gen))
+    return fail(SQ_ERR_INVALID, "no tokens are open (none reserved, or the store changed since)");
+  if (layer < 0 || layer >= s->cfg.num_layers) return fail(SQ_ERR_INVALID, "layer %d out of range", layer);
+  sq::QkArgs a{};
+  sq_status r = take_qk_opts(opts, s->D, &a);
+  if (r != SQ_OK) return r;
+  if ((r = check_rows(q, q_stride, s->cfg.num_q_heads, s->D, "q"))) return r;
+  if ((r = check_rows(k, k_stride, s->cfg.num_kv_heads, s->D, "k"))) return r;
+  if ((r = check_rows(v, v_stride, s->cfg.num_kv_heads, s->D, "v"))) return r;
+  if (!q_out || !aligned16(q_out)) return fail(SQ_ERR_INVALID, "q_out must be non-null and 16-byte aligned");
+  a.q = static_cast<const uint16_t *>(q);
+  a.k = static_cast<const uint16_t *>(k);
+  a.v = static_cast<const uint16_t *>(v);
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.q_out = static_cast<uint16_t *>(q_out);
+  a.pos = s->pools.pos;
+  a.n = op.total;
+  a.hq = s->cfg.num_q_heads;
+  a.hkv = s->cfg.num_kv_heads;
+  a.plan = &s->open_dev->plan;
+  a.ids = s->open_dev->ids;
+  a.n_units = op.n_units;
+  a.k_pool = layer_pool(s, s->pools.k, layer);
+  a.v_pool = layer_pool(s, s->pools.v, layer);
+  a.page_stride = s->pools.page_stride;
+  a.head_stride = s->pools.head_stride;
+  a.kv8 = s->kv8 ? 1 : 0;
+  a.inv_k = s->inv(s->k_scale(layer));
+  a.inv_v = s->inv(s->v_scale(layer));
+  hipStream_t strm = static_cast<hipStream_t>(stream);
+  s->last_stream = strm;
+  ProfPair pp;
+  const bool on = !capturing(strm) && s->prof_begin(strm, &pp, kProfQkv);
+  hipError_t e = sq::launch_qk(s->D, a, strm);
+  s->prof_end(strm, &pp, on);
+  return e == hipSuccess ? SQ_OK : hip_fail(e, "projection store kernel");
+}
+
+sq_status sq_draft_attn(sq_store *s, int32_t layer, const void *q, float *out, float scale,
+                        const sq_attn_opts *opts, void *stream) {
+  SQ_TRACE_CALL("sq_draft_attn", "store=%p layer=%d nodes=%d window=%d sinks=%d", (void *)s, layer, s ? s->open.total : 0, opts ? opts->window : 0, opts && opts->sinks ? 1 : 0);
+  sq_attn_opts o{};
+  sq_status r = take_opts(opts, &o);
+  if (r != SQ_OK) return r;
+  if (!s) return fail(SQ_ERR_INVALID, "null store");
+  if (!s->device) return fail(SQ_ERR_INVALID, "metadata-only store cannot run attention");
+  if ((r = open_draft(s))) return r;
+  const sq_store::Open &op = s->open;
+  if (layer < 0 || layer >= s->cfg.num_layers) return fail(SQ_ERR_INVALID, "layer %d out of range", layer);
+  if (!q || !out || !aligned16(q) || !aligned16(out))
+    return fail(SQ_ERR_INVALID, "q and out must be non-null and 16-byte aligned");
+  if (!std::isfinite(scale) || !(scale > 0.f)) return fail(SQ_ERR_INVALID, "scale must be finite and positive");
+  if (o.window != 0 && (o.window != op.window || o.first != op.first))
+    return fail(SQ_ERR_INVALID, "window %d, first %d: the draft was begun with %d and %d", o.window, o.first,
+                op.window, op.first);
+  sq::DraftArgs a{};
+  a.q = static_cast<const uint16_t *>(q);
+  a.k = layer_pool(s, s->pools.k, layer);
+  a.v = layer_pool(s, s->pools.v, layer);
+  a.out = out;
+  a.pt = s->pt_dev;
+  a.mask = s->mask_dev;
+  a.page_stride = s->pools.page_stride;
+  a.head_stride = s->pools.head_stride;
+  a.max_pages = s->cfg.max_pages_per_seq;
+  a.hq = s->cfg.num_q_heads;
+  a.hkv = s->cfg.num_kv_heads;
+  while ((1 << a.lg) < s->G) ++a.lg;
+  a.total = op.total;
+  a.scale_log2 = (float)((double)scale * 1.4426950408889634 * (double)s->k_scale(layer));
+  a.sinks = o.sinks;
+  a.sink_scale = 1.4426950408889634f;
+  a.out_scale = s->v_scale(layer);
+  a.part_m = s->part_m;
+  a.part_l = s->part_l;
+  a.part_acc = s->part_acc;
+  a.blob = s->open_dev;
+  a.windowed = o.window > 0 ? 1 : 0;
+  a.first = o.window > 0 ? op.first : 0;
+  a.rows = op.rows;
+  a.n_wg = op.n_wg;
+  a.kv8 = s->kv8 ? 1 : 0;
+  hipStream_t strm = static_cast<hipStream_t>(stream);
+  s->last_stream = strm;
+  ProfPair pp;
+  const bool on = !capturing(strm) && s->prof_begin(strm, &pp, kProfDraft);
+  hipError_t e = sq::launch_draft(s->D, a, strm);
+  if (e == hipSuccess) e = sq::launch_draft_merge(s->D, a, strm);
+  s->prof_end(strm, &pp, on);
+  if (e != hipSuccess) return hip_fail(e, "draft attention");
+  ++s->st.draft_calls;
+  s->st.draft_tokens += op.total;
+  s->st.draft_kv_bytes += op.kv_bytes[a.windowed];
+  return SQ_OK;
+}
+
+namespace {
+// Drops the tokens from index `length` on: pages, positions, masks.  The pages'
+// last kept one is the caller's to make private.
+void drop_tail(sq_store *s, Seq &q, int64_t length) {
+  const size_t pages = (size_t)((length + s->P - 1) / s->P);
+  for (size_t i = pages; i < q.pages.size(); ++i) s->unref(q.pages[i], nullptr);
+  q.pages.resize(pages);
+  q.runs = runs_truncate(q.runs, length);
+  q.length = length;
+  if (q.kmask.empty()) return;
+  q.kmask.resize(pages);
+  if (length % s->P) q.kmask.back() |= (uint16_t)(0xffffu << (length % s->P));
+  q.n_masked = 0;
+  for (int64_t pg = 0; pg < (int64_t)pages; ++pg)
+    for (int i = 0; i < s->P; ++i) q.n_masked += !((q.kmask[pg] >> i) & 1);
+  if (q.n_masked == 0) q.kmask.clear();
+}
+} // namespace
+
+sq_status sq_draft_accept(sq_store *s, const int32_t *counts, const int32_t *nodes, void *stream) {
+  SQ_TRACE_CALL("sq_draft_accept", "store=%p batch=%d", (void *)s, s ? (int)s->open.seqs.size() : 0);
+  if (!s || !counts) return fail(SQ_ERR_INVALID, "null argument");
+  sq_status r = open_draft(s);
+  if (r != SQ_OK) return r;
+  sq_store::Open &op = s->open;
+  const int batch = (int)op.seqs.size();
+  sq::AcceptArgs a{};
+  int64_t at = 0, node0 = 0;
+  for (int b = 0; b < batch; ++b) {
+    const int32_t cnt = counts[b];
+    if (cnt < 0 || cnt > op.n[b])
+      return fail(SQ_ERR_INVALID, "%d accepted nodes of sequence %d: it has %d", cnt, op.seqs[b], op.n[b]);
+    if (cnt > 0 && !nodes) return fail(SQ_ERR_INVALID, "null node list");
+    uint64_t mask = 0;
+    for (int32_t j = 0; j < cnt; ++j) {
+      const int32_t i = nodes[at + j];
+      if (i < 0 || i >= op.n[b] || op.parents[node0 + i] != (j == 0 ? -1 : nodes[at + j - 1]))
+        return fail(SQ_ERR_INVALID, "the accepted nodes of sequence %d are no path from a root", op.seqs[b]);
+      mask |= 1ull << i;
+    }
+    if (mask & (mask + 1)) { // not the first nodes in order already
+      a.mask[a.n] = mask;
+      a.row[a.n] = op.seqs[b];
+      a.base[a.n] = (int32_t)op.base[b];
+      a.pos0[a.n] = (int32_t)op.pos0[b];
+      ++a.n;
+    }
+    at += cnt;
+    node0 += op.n[b];
+  }
+  ++s->gen;
+  for (int b = 0; b < batch; ++b) {
+    Seq &q = s->seqs[op.seqs[b]];
+    q.draft = false;
+    q.runs = runs_truncate(q.runs, op.base[b]);
+    q.length = op.base[b];
+    runs_append(q, counts[b]);
+    q.length += counts[b];
+    q.next_pos = op.pos0[b] + counts[b];
+    s->st.append_tokens += counts[b];
+    drop_tail(s, q, q.length);
+  }
+  op = sq_store::Open{};
+  if (!s->device) return SQ_OK;
+  a.max_pages = s->cfg.max_pages_per_seq;
+  a.pt = s->pt_dev;
+  hipStream_t strm = static_cast<hipStream_t>(stream);
+  s->last_stream = strm;
+  hipError_t e = sq::launch_accept(s->pools, a, strm);
+  return e == hipSuccess ? SQ_OK : hip_fail(e, "accept kernel");
+}
+
+sq_status sq_truncate(sq_store *s, sq_seq h, int64_t length, void *stream) {
+  SQ_TRACE_CALL("sq_truncate", "store=%p seq=%d length=%lld", (void *)s, h, (long long)length);
+  if (!s) return fail(SQ_ERR_INVALID, "null store");
+  Seq *q = s->get(h);
+  if (!q) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", h);
+  sq_status r = no_draft(*q, h);
+  if (r != SQ_OK) return r;
+  if (length < 0 || length > q->length)
+    return fail(SQ_ERR_INVALID, "length %lld outside [0, %lld]", (long long)length, (long long)q->length);
+  for (auto &kv : q->spans)
+    if (kv.second.second > length)
+      return fail(SQ_ERR_SPAN, "cursor %d ends at %lld, past %lld", kv.first, (long long)kv.second.second,
+                  (long long)length);
+  if (length == q->length) return SQ_OK;
+  // the tokens appended next go into a part-full last page: it must be the
+  // sequence's own
+  const int64_t full = length / s->P;
+  const bool copy = length % s->P && s->refcount[q->pages[full]] > 1;
+  if (copy && s->n_free < 1) return fail(SQ_ERR_NO_PAGES, "no page for the copy of the shared last page");
+  ++s->gen;
+  const int64_t masked = q->n_masked;
+  q->next_pos = pos_at(*q, length);
+  const int32_t from = copy ? q->pages[full] : -1;
+  int32_t to = -1;
+  if (copy) {
+    to = s->alloc_page();
+    s->unref(from, nullptr);
+    q->pages[full] = to;
+  }
+  drop_tail(s, *q, length);
+  if (!s->device) return SQ_OK;
+  hipStream_t strm = static_cast<hipStream_t>(stream);
+  if (copy) {
+    s->last_stream = strm;
+    hipError_t e = sq::launch_fork(s->pools, s->pt_row(h) + full, s->pt_row(h) + full, 0, from, to, strm);
+    if (e != hipSuccess) return hip_fail(e, "truncate");
+  }
+  if (q->n_masked > 0 && q->n_masked != masked) { // dropped slots take unmasked tokens next
+    s->last_stream = strm;
+    return upload_mask_row(s, h, strm);
+  }
+  return SQ_OK;
+}
+
 sq_status sq_decode_plan_info(sq_store *s, const sq_seq *seqs, int32_t batch, int32_t mode,
                               sq_plan_info *out) {
   if (!s || !seqs || !out) return fail(SQ_ERR_INVALID, "null argument");
@@ -1969,11 +2598,20 @@ sq_status sq_step_begin(sq_store *s, const sq_seq *seqs, int32_t batch, int32_t 
 
 sq_status sq_step_begin_ex(sq_store *s, const sq_seq *seqs, int32_t batch, int32_t mode,
                            int32_t window, void *stream) {
-  SQ_TRACE_CALL("sq_step_begin", "store=%p batch=%d mode=%d window=%d", (void *)s, batch, mode, window);
+  sq_attn_opts o{};
+  o.window = window;
+  return sq_step_begin_opts(s, seqs, batch, mode, &o, stream);
+}
+
+sq_status sq_step_begin_opts(sq_store *s, const sq_seq *seqs, int32_t batch, int32_t mode,
+                             const sq_attn_opts *opts, void *stream) {
+  SQ_TRACE_CALL("sq_step_begin", "store=%p batch=%d mode=%d window=%d first=%d", (void *)s, batch, mode, opts ? opts->window : 0, opts ? opts->first : 0);
   sq_status r = check_one_token_each(s, seqs, batch);
   if (r != SQ_OK) return r;
+  sq_attn_opts o{};
+  if ((r = take_opts(opts, &o))) return r;
+  const int32_t window = o.window;
   if (mode < SQ_ATTN_AUTO || mode > SQ_ATTN_MFMA) return fail(SQ_ERR_INVALID, "unknown mode %d", mode);
-  if (window < 0) return fail(SQ_ERR_INVALID, "window %d < 0", window);
   // attention over the tokens before the step; the new ones join in the
   // merge (a window of W keys: the new token and the last W - 1 old ones)
   Plan plan, plan_w;
@@ -1982,7 +2620,7 @@ sq_status sq_step_begin_ex(sq_store *s, const sq_seq *seqs, int32_t batch, int32
   if (window > 0) {
     if (plan.masked)
       return fail(SQ_ERR_INVALID, "a window over a sequence with masked slots (compact it first)");
-    r = build_plan(s, seqs, batch, mode, &plan_w, window - 1);
+    r = build_plan(s, seqs, batch, mode, &plan_w, window - 1, 1, o.first);
     if (r != SQ_OK) return r;
   }
   // which launches a layer makes depends on the mode only, so that a
@@ -2040,6 +2678,7 @@ sq_status sq_step_begin_ex(sq_store *s, const sq_seq *seqs, int32_t batch, int32
   st.kv_bytes = plan.kv_bytes + batch * tok_bytes;
   st.kv_bytes_logical = plan.kv_bytes_logical + batch * tok_bytes;
   st.window = window;
+  st.first = o.first;
   st.kv_bytes_w = plan_w.kv_bytes + batch * tok_bytes;
   st.kv_bytes_logical_w = plan_w.kv_bytes_logical + batch * tok_bytes;
   if (!s->device) return SQ_OK;
@@ -2093,6 +2732,8 @@ sq_status sq_step_attn_ex(sq_store *s, int32_t layer, const void *k_new, const v
   if (!std::isfinite(scale)) return fail(SQ_ERR_INVALID, "scale must be finite");
   if (o.window != 0 && o.window != st.window)
     return fail(SQ_ERR_INVALID, "window %d: the step was begun with window %d", o.window, st.window);
+  if (o.window != 0 && o.first != st.first)
+    return fail(SQ_ERR_INVALID, "first %d: the step was begun with first %d", o.first, st.first);
   const bool win = o.window != 0;
   hipStream_t strm = static_cast<hipStream_t>(stream);
   s->last_stream = strm;
@@ -2154,6 +2795,7 @@ sq_status sq_extend_attn_ex(sq_store *s, int32_t layer, sq_seq seq, int32_t n_ne
   if (!sqn) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", seq);
   if (n_new < 0 || n_new > sqn->length)
     return fail(SQ_ERR_INVALID, "n_new %d outside [0, %lld]", n_new, (long long)sqn->length);
+  if ((r = no_draft(*sqn, seq))) return r;
   if (n_new == 0) return SQ_OK;
   if (!q || !out || !aligned16(q) || !aligned16(out))
     return fail(SQ_ERR_INVALID, "q and out must be non-null and 16-byte aligned");
@@ -2177,6 +2819,7 @@ sq_status sq_extend_attn_ex(sq_store *s, int32_t layer, sq_seq seq, int32_t n_ne
   a.scale_log2 = (float)((double)scale * 1.4426950408889634 * (double)s->k_scale(layer));
   a.sinks = o.sinks;
   a.window = o.window;
+  a.first = o.window > 0 ? o.first : 0;
   a.sink_scale = 1.4426950408889634f;
   a.kv8 = s->kv8 ? 1 : 0;
   a.out_scale = s->v_scale(layer);
@@ -2184,7 +2827,7 @@ sq_status sq_extend_attn_ex(sq_store *s, int32_t layer, sq_seq seq, int32_t n_ne
   a.masked = sqn->n_masked > 0 ? 1 : 0;
   if (a.masked && o.window > 0)
     return fail(SQ_ERR_INVALID, "a window over a sequence with masked slots (compact it first)");
-  const ExtendPlan ep = plan_extend(s, n_new, sqn->length, o.window);
+  const ExtendPlan ep = plan_extend(s, n_new, sqn->length, o.window, a.first);
   a.rows = ep.rows;
   a.n_qblocks = ep.n_qblocks;
   a.n_split = ep.n_split;
@@ -2200,7 +2843,7 @@ sq_status sq_extend_attn_ex(sq_store *s, int32_t layer, sq_seq seq, int32_t n_ne
   if (e != hipSuccess) return hip_fail(e, "extend kernel");
   ++s->st.extend_calls;
   s->st.extend_tokens += n_new;
-  const int64_t keys_read = o.window > 0 ? std::min<int64_t>(sqn->length, (int64_t)n_new + o.window - 1)
+  const int64_t keys_read = o.window > 0 ? std::min<int64_t>(sqn->length, (int64_t)n_new + o.window - 1 + a.first)
                                          : sqn->length;
   s->st.extend_kv_bytes += keys_read * (int64_t)s->cfg.num_kv_heads * s->D * 2 * s->elem_bytes();
   return SQ_OK;
@@ -2354,6 +2997,10 @@ sq_status sq_profile_read(sq_store *s, sq_profile *out) {
   out->append_launches = s->prof_n[kProfAppend];
   out->extend_ms = s->prof_ms[kProfExtend];
   out->extend_launches = s->prof_n[kProfExtend];
+  out->qkv_ms = s->prof_ms[kProfQkv];
+  out->qkv_launches = s->prof_n[kProfQkv];
+  out->draft_ms = s->prof_ms[kProfDraft];
+  out->draft_launches = s->prof_n[kProfDraft];
   for (int k = 0; k < kProfKinds; ++k) {
     s->prof_ms[k] = 0;
     s->prof_n[k] = 0;

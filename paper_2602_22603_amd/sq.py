@@ -25,6 +25,8 @@ EVICT_DEFER = 1
 ATTN_AUTO, ATTN_STREAM, ATTN_SHARED_PREFIX, ATTN_MFMA = 0, 1, 2, 3
 MAX_BATCH = 64
 MAX_EVICT_SPANS = 16384
+MAX_RESERVE = 262144
+MAX_DRAFT = 64
 
 _STATUS_NAMES = {
     ERR_INVALID: "SQ_ERR_INVALID", ERR_NO_PAGES: "SQ_ERR_NO_PAGES",
@@ -66,7 +68,8 @@ class Stats(C.Structure):
         "live_pages", "peak_pages", "free_pages", "live_seqs", "append_tokens",
         "fork_calls", "fork_tail_copies", "evict_calls", "evict_tokens_removed",
         "evict_tokens_moved", "evict_bytes_moved", "decode_calls", "decode_kv_bytes",
-        "decode_kv_bytes_logical", "extend_calls", "extend_tokens", "extend_kv_bytes")]
+        "decode_kv_bytes_logical", "extend_calls", "extend_tokens", "extend_kv_bytes",
+        "draft_calls", "draft_tokens", "draft_kv_bytes")]
 
 
 class PlanInfo(C.Structure):
@@ -83,7 +86,14 @@ class ExtendInfo(C.Structure):
 
 
 class AttnOpts(C.Structure):
-    _fields_ = [("sinks", C.c_void_p), ("window", C.c_int32), ("reserved", C.c_int32)]
+    _fields_ = [("sinks", C.c_void_p), ("window", C.c_int32), ("reserved", C.c_int32),
+                ("first", C.c_int32), ("reserved2", C.c_int32)]
+
+
+class QkOpts(C.Structure):
+    _fields_ = [("inv_freq", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p),
+                ("eps", C.c_float), ("mscale", C.c_float), ("rot_dim", C.c_int32),
+                ("interleaved", C.c_int32)]
 
 
 class Profile(C.Structure):
@@ -92,7 +102,9 @@ class Profile(C.Structure):
                 [(n, C.c_int64) for n in ("decode_valu_launches", "decode_mfma_launches",
                                            "decode_merge_launches", "evict_scan_launches",
                                            "evict_gather_launches", "append_launches")] +
-                [("extend_ms", C.c_double), ("extend_launches", C.c_int64)])
+                [("extend_ms", C.c_double), ("extend_launches", C.c_int64)] +
+                [(n, C.c_double) for n in ("qkv_ms", "draft_ms")] +
+                [(n, C.c_int64) for n in ("qkv_launches", "draft_launches")])
 
 
 _LIB = None
@@ -140,6 +152,22 @@ _SIGS = {
                                    C.c_int32, C.c_void_p]),
     "sq_step_attn_ex": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                                   C.c_void_p, C.c_float, C.POINTER(AttnOpts), C.c_void_p]),
+    "sq_step_begin_opts": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.c_int32, C.c_int32,
+                                     C.POINTER(AttnOpts), C.c_void_p]),
+    "sq_qk_rope": (C.c_int, [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int32,
+                             C.c_int32, C.c_int32, C.c_int32, C.POINTER(QkOpts), C.c_void_p,
+                             C.c_void_p, C.c_void_p]),
+    "sq_reserve": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32,
+                             C.c_void_p]),
+    "sq_qkv_store": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                               C.c_void_p, C.c_int64, C.POINTER(QkOpts), C.c_void_p, C.c_void_p]),
+    "sq_truncate": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p]),
+    "sq_draft_begin": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.c_int32,
+                                 C.POINTER(C.c_int32), C.POINTER(AttnOpts), C.c_void_p]),
+    "sq_draft_attn": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_float,
+                                C.POINTER(AttnOpts), C.c_void_p]),
+    "sq_draft_accept": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.POINTER(C.c_int32),
+                                  C.c_void_p]),
     "sq_decode_plan_info": (C.c_int, [C.c_void_p, C.POINTER(C.c_int32), C.c_int32, C.c_int32,
                                       C.POINTER(PlanInfo)]),
     "sq_extend_plan_info": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
@@ -214,6 +242,89 @@ def _stream(stream):
     if isinstance(stream, int):
         return C.c_void_p(stream)
     return C.c_void_p(stream.cuda_stream)
+
+
+def _rows(t, heads, dim, dev, what):
+    """(pointer, row stride) of bf16 [n, heads, dim] whose tokens may lie apart
+    (a view of a fused projection), on device dev."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
+        raise SqError(ERR_INVALID, f"{what} must be a bfloat16 tensor")
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim:
+        raise SqError(ERR_INVALID, f"{what} must have shape (n, {heads}, {dim}), got {tuple(t.shape)}")
+    st = t.stride()
+    if st[2] != 1 or (heads > 1 and st[1] != dim):
+        raise SqError(ERR_INVALID, f"{what}: the heads of a token must be contiguous")
+    if t.device != dev:
+        raise SqError(ERR_INVALID, f"{what} must be on {dev}, got {t.device}")
+    return t.data_ptr(), st[0] if t.shape[0] > 1 else heads * dim
+
+
+def _packed(t, shape, dtype, dev, what):
+    """Pointer of a contiguous tensor of exactly this shape and dtype on dev."""
+    import torch
+    if not isinstance(t, torch.Tensor) or t.dtype != dtype:
+        raise SqError(ERR_INVALID, f"{what} must be a {dtype} tensor")
+    if tuple(t.shape) != shape or not t.is_contiguous():
+        raise SqError(ERR_INVALID, f"{what} must be contiguous of shape {shape}, got {tuple(t.shape)}")
+    if t.device != dev:
+        raise SqError(ERR_INVALID, f"{what} must be on {dev}, got {t.device}")
+    return t.data_ptr()
+
+
+def _current(dev):
+    """The library launches on the current device, where its buffers must be."""
+    import torch
+    if dev.type != "cuda" or dev.index not in (None, torch.cuda.current_device()):
+        raise SqError(ERR_INVALID, f"tensors on {dev}: make it the current device")
+
+
+def _qk_opts(dim, dev, inv_freq, q_weight, k_weight, eps, interleaved, mscale):
+    """QkOpts, or None when there is nothing to do."""
+    import torch
+    if inv_freq is None and q_weight is None and k_weight is None:
+        return None
+    o = QkOpts(eps=float(eps), mscale=float(mscale), interleaved=1 if interleaved else 0)
+    if inv_freq is not None:
+        n = int(inv_freq.shape[0]) if inv_freq.dim() == 1 else -1
+        o.inv_freq = _packed(inv_freq, (n,), torch.float32, dev, "inv_freq")
+        o.rot_dim = 2 * n
+    if q_weight is not None:
+        o.q_weight = _packed(q_weight, (dim,), torch.float32, dev, "q_weight")
+    if k_weight is not None:
+        o.k_weight = _packed(k_weight, (dim,), torch.float32, dev, "k_weight")
+    return o
+
+
+def qk_rope(q, k, positions, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6,
+            interleaved=False, mscale=1.0, q_out=None, k_out=None, stream=None):
+    """Norm of every query and key head and position rotation in one pass
+    (sq_qk_rope): q bf16 [n, Hq, D], k bf16 [n, Hkv, D], whose tokens may lie
+    apart; positions int32 [n]; inv_freq fp32 [rot_dim / 2] (None: no
+    rotation); q_weight, k_weight fp32 [D] (None: no norm).  Returns (q_out,
+    k_out), bf16 and packed; they may be q and k where those are packed."""
+    import torch
+    if not isinstance(q, torch.Tensor) or q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise SqError(ERR_INVALID, "q and k must be tensors of three dimensions")
+    dev = q.device
+    _current(dev)
+    n, hq, dim = q.shape
+    hkv = k.shape[1]
+    if k.shape[0] != n:
+        raise SqError(ERR_INVALID, f"k must have {n} tokens, got {k.shape[0]}")
+    if q_out is None:
+        q_out = torch.empty((n, hq, dim), dtype=torch.bfloat16, device=dev)
+    if k_out is None:
+        k_out = torch.empty((n, hkv, dim), dtype=torch.bfloat16, device=dev)
+    qp, qs = _rows(q, hq, dim, dev, "q")
+    kp, ks = _rows(k, hkv, dim, dev, "k")
+    qo = _packed(q_out, (n, hq, dim), torch.bfloat16, dev, "q_out")
+    ko = _packed(k_out, (n, hkv, dim), torch.bfloat16, dev, "k_out")
+    pos = _packed(positions, (n,), torch.int32, dev, "positions")
+    o = _qk_opts(dim, dev, inv_freq, q_weight, k_weight, eps, interleaved, mscale)
+    _check(lib().sq_qk_rope(qp, qs, kp, ks, pos, n, hq, hkv, dim, None if o is None else C.byref(o),
+                            qo, ko, _stream(stream)))
+    return q_out, k_out
 
 
 class Store:
@@ -319,14 +430,15 @@ class Store:
         return (self._tensor(k_new, shape, torch.bfloat16, "k_new"),
                 self._tensor(v_new, shape, torch.bfloat16, "v_new"))
 
-    def _opts(self, window, sinks):
-        """AttnOpts for (window, sinks) or None when neither is set; sinks is
-        a float32 tensor [Hq] on the store's device."""
+    def _opts(self, window, sinks, first=0):
+        """AttnOpts for (window, sinks, first) or None when none is set; sinks
+        is a float32 tensor [Hq] on the store's device."""
         import torch
-        if not window and sinks is None:
+        if not window and sinks is None and not first:
             return None
         o = AttnOpts()
         o.window = int(window)
+        o.first = int(first)
         if sinks is not None:
             o.sinks = (_ptr(sinks) if self.metadata_only else
                        self._tensor(sinks, (self.num_q_heads,), torch.float32, "sinks"))
@@ -401,9 +513,10 @@ class Store:
         return buf[: n.value]
 
     def decode(self, layer, seqs, q, out=None, scale=None, mode=ATTN_AUTO, stream=None,
-               window=0, sinks=None):
+               window=0, sinks=None, first=0):
         """out[b, h] = attention of q[b, h] (bf16 [B, Hq, D]) over seqs[b]; fp32.
-        window > 0: the last `window` keys only; sinks: fp32 [Hq] sink logits."""
+        window > 0: the last `window` keys only, and the first `first` ones;
+        sinks: fp32 [Hq] sink logits."""
         import torch
         if out is None:
             out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
@@ -411,7 +524,7 @@ class Store:
             scale = 1.0 / float(self.head_dim) ** 0.5
         seqs = list(seqs)
         qp, op = (_ptr(q), _ptr(out)) if self.metadata_only else self._qo_ptrs(q, out, len(seqs))
-        o = self._opts(window, sinks)
+        o = self._opts(window, sinks, first)
         if o is None:
             _check(lib().sq_decode_attn(self._handle, layer, _i32_array(seqs), len(seqs), qp, op,
                                         float(scale), mode, _stream(stream)))
@@ -432,17 +545,22 @@ class Store:
                                             op, float(scale), mode, _stream(stream)))
         return out
 
-    def step_begin(self, seqs, mode=ATTN_AUTO, stream=None, window=0):
+    def step_begin(self, seqs, mode=ATTN_AUTO, stream=None, window=0, first=0):
         """Open a decode step: one token slot appended to each of seqs (their
         K/V arrive layer by layer through step_attn).  window > 0 also plans
-        layers that attend to the last `window` keys only."""
+        layers that attend to the last `window` keys only, and to the first
+        `first` ones."""
         seqs = list(seqs)
         st = C.c_void_p(0) if self.metadata_only else _stream(stream)
         # the C side trusts buffer sizes: step_attn checks them against the
         # batch of the last step this binding opened, and refuses after a
         # failed step_begin
         self._step_batch = None
-        if window:
+        if first:
+            o = self._opts(window, None, first)
+            _check(lib().sq_step_begin_opts(self._handle, _i32_array(seqs), len(seqs), mode,
+                                            C.byref(o), st))
+        elif window:
             _check(lib().sq_step_begin_ex(self._handle, _i32_array(seqs), len(seqs), mode,
                                           int(window), st))
         else:
@@ -450,11 +568,11 @@ class Store:
         self._step_batch = len(seqs)
 
     def step_attn(self, layer, k_new, v_new, q, out=None, scale=None, stream=None, window=0,
-                  sinks=None):
+                  sinks=None, first=0):
         """One layer of the open step: store k_new, v_new (bf16 [B, Hkv, D])
         and attend with q (bf16 [B, Hq, D]) over every token, the new one
-        included; returns out (fp32 [B, Hq, D]).  window: 0 or the step's
-        window; sinks: fp32 [Hq] sink logits."""
+        included; returns out (fp32 [B, Hq, D]).  window, first: 0 or the
+        step's; sinks: fp32 [Hq] sink logits."""
         import torch
         if out is None:
             out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
@@ -469,7 +587,7 @@ class Store:
             kv = (b, self.num_kv_heads, self.head_dim)
             ptrs = (self._tensor(k_new, kv, torch.bfloat16, "k_new"),
                     self._tensor(v_new, kv, torch.bfloat16, "v_new"), *self._qo_ptrs(q, out, b))
-        o = self._opts(window, sinks)
+        o = self._opts(window, sinks, first)
         if o is None:
             _check(lib().sq_step_attn(self._handle, layer, *ptrs, float(scale), _stream(stream)))
         else:
@@ -477,10 +595,12 @@ class Store:
                                          _stream(stream)))
         return out
 
-    def extend(self, layer, seq, q, out=None, scale=None, stream=None, window=0, sinks=None):
+    def extend(self, layer, seq, q, out=None, scale=None, stream=None, window=0, sinks=None,
+               first=0):
         """Causal attention of the last n = q.shape[0] tokens of seq (just
         appended) over the cache: q bf16 [n, Hq, D] -> out fp32 [n, Hq, D].
-        window > 0: each token sees its last `window` keys; sinks: fp32 [Hq]."""
+        window > 0: each token sees its last `window` keys and the first
+        `first` ones; sinks: fp32 [Hq]."""
         import torch
         if out is None:
             out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
@@ -488,7 +608,7 @@ class Store:
             scale = 1.0 / float(self.head_dim) ** 0.5
         n = int(q.shape[0])
         qp, op = (_ptr(q), _ptr(out)) if self.metadata_only else self._qo_ptrs(q, out, n)
-        o = self._opts(window, sinks)
+        o = self._opts(window, sinks, first)
         if o is None:
             _check(lib().sq_extend_attn(self._handle, layer, seq, n, qp, op, float(scale),
                                         _stream(stream)))
@@ -496,6 +616,105 @@ class Store:
             _check(lib().sq_extend_attn_ex(self._handle, layer, seq, n, qp, op, float(scale),
                                            C.byref(o), _stream(stream)))
         return out
+
+    # -- tokens whose K and V come layer by layer ----------------------------------
+    def reserve(self, seqs, counts, stream=None):
+        """Append counts[b] token slots to each of seqs; their K and V come
+        layer by layer (qkv_store)."""
+        seqs, counts = list(seqs), list(counts)
+        if len(seqs) != len(counts):
+            raise SqError(ERR_INVALID, "one count for each sequence")
+        if not self.metadata_only:
+            _current(self.k_pool.device)
+        st = C.c_void_p(0) if self.metadata_only else _stream(stream)
+        _check(lib().sq_reserve(self._handle, _i32_array(seqs), _i32_array(counts), len(seqs), st))
+        self._open_tokens = sum(counts)
+
+    def qkv_store(self, layer, q, k, v, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6,
+                  interleaved=False, mscale=1.0, q_out=None, stream=None):
+        """A layer's projections of the open tokens (reserve, draft_begin): q
+        normed and rotated to q_out (bf16 [n, Hq, D]), k and v into the
+        tokens' slots.  q, k, v bf16 [n, heads, D], tokens may lie apart; the
+        rest as for qk_rope.  Returns q_out."""
+        import torch
+        if self.metadata_only:
+            raise SqError(ERR_INVALID, "metadata-only store holds no K and V")
+        dev = self.k_pool.device
+        _current(dev)
+        n = getattr(self, "_open_tokens", None)
+        if n is None:
+            raise SqError(ERR_INVALID, "no tokens opened by this binding")
+        hq, hkv, dim = self.num_q_heads, self.num_kv_heads, self.head_dim
+        qp, qs = _rows(q, hq, dim, dev, "q")
+        kp, ks = _rows(k, hkv, dim, dev, "k")
+        vp, vs = _rows(v, hkv, dim, dev, "v")
+        for t, what in ((q, "q"), (k, "k"), (v, "v")):
+            if t.shape[0] != n:
+                raise SqError(ERR_INVALID, f"{what} must have {n} tokens, got {t.shape[0]}")
+        if q_out is None:
+            q_out = torch.empty((n, hq, dim), dtype=torch.bfloat16, device=dev)
+        qo = _packed(q_out, (n, hq, dim), torch.bfloat16, dev, "q_out")
+        o = _qk_opts(dim, dev, inv_freq, q_weight, k_weight, eps, interleaved, mscale)
+        _check(lib().sq_qkv_store(self._handle, layer, qp, qs, kp, ks, vp, vs,
+                                  None if o is None else C.byref(o), qo, _stream(stream)))
+        return q_out
+
+    def truncate(self, seq, length, stream=None):
+        """Drop the tokens of seq from index `length` on."""
+        st = C.c_void_p(0) if self.metadata_only else _stream(stream)
+        _check(lib().sq_truncate(self._handle, seq, int(length), st))
+
+    # -- drafted tokens ------------------------------------------------------------
+    def draft_begin(self, seqs, parents, window=0, first=0, stream=None):
+        """Open a draft: parents[b] lists the parent of every node of seqs[b]'s
+        tree (an earlier node, or -1).  window, first: of the layers that will
+        be windowed."""
+        seqs = list(seqs)
+        counts = [len(p) for p in parents]
+        if len(seqs) != len(counts):
+            raise SqError(ERR_INVALID, "one tree for each sequence")
+        if not self.metadata_only:
+            _current(self.k_pool.device)
+        o = self._opts(window, None, first)
+        st = C.c_void_p(0) if self.metadata_only else _stream(stream)
+        _check(lib().sq_draft_begin(self._handle, _i32_array(seqs), _i32_array(counts), len(seqs),
+                                    _i32_array([x for p in parents for x in p]),
+                                    None if o is None else C.byref(o), st))
+        self._open_tokens = sum(counts)
+        self._draft_seqs = len(seqs)
+
+    def draft_attn(self, layer, q, out=None, scale=None, window=0, first=0, sinks=None, stream=None):
+        """One layer's attention of the open draft's nodes over their
+        sequences and ancestors: q bf16 [nodes, Hq, D] -> out fp32 alike.
+        window, first: 0 or the begin's; sinks: fp32 [Hq]."""
+        import torch
+        if self.metadata_only:
+            raise SqError(ERR_INVALID, "metadata-only store cannot run attention")
+        n = getattr(self, "_open_tokens", None)
+        if n is None:
+            raise SqError(ERR_INVALID, "no tokens opened by this binding")
+        _current(self.k_pool.device)
+        if out is None:
+            out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        if scale is None:
+            scale = 1.0 / float(self.head_dim) ** 0.5
+        qp, op = self._qo_ptrs(q, out, n)
+        o = self._opts(window, sinks, first if window else 0)
+        _check(lib().sq_draft_attn(self._handle, layer, qp, op, float(scale),
+                                   None if o is None else C.byref(o), _stream(stream)))
+        return out
+
+    def draft_accept(self, paths, stream=None):
+        """Keep paths[b] (nodes from a root on; empty: none) of each sequence of
+        the open draft, drop its other nodes and end it."""
+        paths = [list(p) for p in paths]
+        if len(paths) != getattr(self, "_draft_seqs", 0):
+            raise SqError(ERR_INVALID, "one path for each sequence of the open draft")
+        st = C.c_void_p(0) if self.metadata_only else _stream(stream)
+        _check(lib().sq_draft_accept(self._handle, _i32_array([len(p) for p in paths]),
+                                     _i32_array([x for p in paths for x in p]), st))
+        self._open_tokens = None
+        self._draft_seqs = 0
 
     def plan_info(self, seqs, mode=ATTN_AUTO):
         pi = PlanInfo()
