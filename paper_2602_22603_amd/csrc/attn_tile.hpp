@@ -172,7 +172,8 @@ __device__ inline __amdgpu_buffer_rsrc_t ext_page(const void *page, int bytes) {
 // block, or a part of one, K rows and V^T alike, so one page address (formed by
 // the scalar unit from the page id) serves all copy instructions of a page and
 // the lanes add offsets that do not change from block to block.
-template <int D, int W, class PG>
+// AUX: the loads' cache policy (2: non-temporal, for keys that are read once).
+template <int D, int W, int AUX = 0, class PG>
 __device__ inline void ext_dma(uint16_t *sk, uint16_t *sv, const PG &a,
                                const uint16_t *kbase, const uint16_t *vbase,
                                const int32_t (&ids)[4], int wave, int lane) {
@@ -190,13 +191,13 @@ __device__ inline void ext_dma(uint16_t *sk, uint16_t *sv, const PG &a,
       const int row = ins * Lt::KROWS + lane / Lt::CH;
       const int c = k_phys<D>(row, lane % Lt::CH); // the swizzle is an involution
       __builtin_amdgcn_raw_ptr_buffer_load_lds(kr, (lds_void *)(sk + ins * 512), 16,
-                                               ((row % kPage) * D + 8 * c) * 2, 0, 0, 0);
+                                               ((row % kPage) * D + 8 * c) * 2, 0, 0, AUX);
     }
 #pragma unroll
     for (int u = pg * PER; u < (pg + 1) * PER; ++u) {
       const int ins = wave * Lt::NV + u;
       __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (lds_void *)(sv + ins * 512), 16,
-                                               ((ins % IPP) * 512 + lane * 8) * 2, 0, 0, 0);
+                                               ((ins % IPP) * 512 + lane * 8) * 2, 0, 0, AUX);
     }
   }
 }

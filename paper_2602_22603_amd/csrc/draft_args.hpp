@@ -10,45 +10,49 @@
 
 namespace sq {
 
-// A tile is up to rows / G nodes of one sequence with the G query heads of a KV
-// head; a row of the plan is (tile, KV head).  Its keys are nb blocks of 64: of
-// a windowed plan the blocks of the first tokens, then (nf blocks on) those from
-// the window's start, skip blocks later.
-struct DraftTile {
-  int32_t row;      // page-table row
-  int32_t base;     // tokens in front of the draft
-  int32_t n;        // nodes of the sequence
-  int32_t n_pages;
-  int32_t node0;    // first node of the tile, among all
-  int32_t n_nodes;  // nodes of the tile
-  int32_t masked;   // the sequence has slots masked by deferred evictions
-  int32_t pad;
-  int32_t nf[2], skip[2], lo_max[2]; // full plan, windowed plan
-  int32_t pad2[2];
-};
 // What a node sees: of the draft the nodes of anc (bit i: node i), of the cache
 // the tokens from lo on and, in the windowed plan, the first tokens.
 struct DraftNode {
-  uint64_t anc[2];
-  int32_t lo;   // windowed plan
-  int32_t tile;
+  uint64_t anc[2]; // full plan, windowed plan
+  int32_t lo;      // windowed plan
+  int32_t tile;    // its tile, and its place in it
+  int32_t in_tile;
+  int32_t pad;
 };
-// Blocks [b_lo, b_hi) (counted as in the tile) of a row, by one workgroup: the
-// whole row's (slot < 0: to the output), or a part of it (a partial slot).
+// A tile is up to rows / G nodes of one sequence with the G query heads of a KV
+// head; a row of the plan is (tile, KV head).  Its keys are a list of blocks of
+// 64: of a windowed plan the blocks of the first tokens, then (from place nf on)
+// those from the window's start, `skip` blocks later.  A piece is a run of one
+// row's blocks, for one workgroup: with all that the workgroup has to know, so
+// that it starts after one load.  Workgroup w's first piece is piece w.
 struct DraftPiece {
-  int32_t row, b_lo, b_hi, slot;
+  int32_t g;          // KV head
+  int32_t row;        // page-table row
+  int32_t base;       // tokens in front of the draft
+  int32_t n;          // nodes of the sequence
+  int32_t n_pages;
+  int32_t node0;      // first node of the tile, among all
+  int32_t n_nodes;    // nodes of the tile
+  int32_t masked;     // the sequence has slots masked by deferred evictions
+  int32_t nf, skip;
+  int32_t lo_max;     // where the last node's window starts
+  int32_t b_lo, b_hi; // places in the list
+  int32_t slot;       // first partial row of a part of the blocks, or -1: to the output
+  int32_t next;       // the workgroup's next piece, or -1
+  int32_t pad;
 };
-// The partial slots of a row (none: written by its one piece).
+// The partial rows of a row's n pieces, one tile's rows apart (n = 0: written by
+// its one piece).
 struct DraftMerge {
-  int32_t slot0, n;
+  int32_t row0, n;
 };
 
-constexpr int kDraftTiles = 2 * kMaxBatch;
-constexpr int kDraftRows = 4096;       // (tile, KV head) rows
-constexpr int kDraftWgs = 1024;        // workgroups of a launch
+constexpr int kDraftTiles = 4 * kMaxBatch;
+constexpr int kDraftRows = 4096; // (tile, KV head) rows
+constexpr int kDraftWgs = 1024;  // workgroups of a launch
 struct DraftSplit {
+  int32_t n_used, pad[3];        // workgroups that have work
   DraftMerge merge[kDraftRows];
-  int32_t piece0[kDraftWgs + 4];
   DraftPiece pieces[kDraftRows + kDraftWgs];
 };
 // The blob in device memory (and, pinned, on the host), uploaded in the parts
@@ -57,14 +61,13 @@ struct OpenBlob {
   OpenPlan plan;
   int32_t ids[kOpenMaxUnits];
   int32_t depth[kMaxBatch * kMaxDraft];
-  DraftTile tiles[kDraftTiles];
   DraftNode nodes[kMaxBatch * kMaxDraft];
   DraftSplit split[2]; // every key; a window
 };
 static_assert(sizeof(OpenPlan) % 16 == 0 && offsetof(OpenBlob, ids) % 16 == 0 && offsetof(OpenBlob, depth) % 16 == 0 &&
-                  offsetof(OpenBlob, tiles) % 16 == 0 && offsetof(OpenBlob, nodes) % 16 == 0 &&
-                  offsetof(OpenBlob, split) % 16 == 0 && sizeof(DraftSplit) % 16 == 0 &&
-                  offsetof(DraftSplit, piece0) % 16 == 0 && offsetof(DraftSplit, pieces) % 16 == 0,
+                  offsetof(OpenBlob, nodes) % 16 == 0 && offsetof(OpenBlob, split) % 16 == 0 &&
+                  sizeof(DraftSplit) % 16 == 0 && offsetof(DraftSplit, merge) % 16 == 0 &&
+                  offsetof(DraftSplit, pieces) % 16 == 0,
               "uploaded as 16-byte units");
 
 struct DraftArgs {
@@ -84,12 +87,13 @@ struct DraftArgs {
   const float *sinks;
   float sink_scale;
   float out_scale;
-  float *part_m, *part_l, *part_acc; // [slots][rows], acc [slots][rows][D]
+  float *part_m, *part_l, *part_acc; // [partial rows], acc [partial rows][D]
   const OpenBlob *blob;
   int32_t windowed;  // which plan
   int32_t first;     // first tokens beside the window
-  int32_t rows;      // query rows per workgroup: 256, 128 or 64
+  int32_t rows;      // query rows per workgroup: 256, 128 or 64 (8-bit stores also 32 or 16)
   int32_t n_wg;
+  int32_t shared;    // a sequence may have several tiles, which read the same keys
   int32_t kv8;
 };
 static_assert(sizeof(DraftArgs) < 4096, "draft kernel arguments too large");

@@ -409,7 +409,7 @@ struct sq_store {
     std::vector<int32_t> parents; // a draft's, entry after entry
     int32_t total = 0, n_units = 0;
     int32_t window = 0, first = 0;
-    int32_t rows = 0, n_wg = 0;
+    int32_t rows = 0, n_wg = 0, shared = 0; // a draft's launches
     int64_t kv_bytes[2] = {0, 0};
   } open;
 
@@ -1978,50 +1978,105 @@ sq_status sq_evict_spans_ex(sq_store *s, sq_seq h, const int32_t *cursor_ids, in
 // ---- tokens whose K and V come layer by layer --------------------------------
 namespace {
 
-// The shape of a draft's work: query rows per workgroup and workgroups of a
-// launch.  They follow from the counts alone, so that a captured layer replays
-// for later drafts of the same counts.  A tile of 256 rows (eight waves, one
-// workgroup a CU), 128 or 64 (two a CU) is the smallest that holds the largest
-// tree's rows; more than 256 take two tiles.
-void draft_shape(const sq_store *s, int32_t most_nodes, int32_t *rows, int32_t *n_wg) {
-  const int r = most_nodes * s->G;
-  *rows = r <= 64 ? 64 : r <= 128 ? 128 : 256;
-  const int64_t wg = (int64_t)s->cus * (*rows == 256 ? 1 : 2);
-  // every workgroup may leave two partial slots of `rows` rows
-  *n_wg = (int32_t)std::min<int64_t>({wg, sq::kDraftWgs, (int64_t)sq::kMaxItems * sq::kRows / *rows / 2});
+// How a draft's work is cut: query rows per workgroup, and workgroups of a launch
+// (one round: two waves a SIMD, fewer where the LDS says so).  It follows from
+// the counts alone, so that a captured layer replays for later drafts of the same
+// counts.  A wave takes 32 rows, so the tile is the smallest that holds the
+// largest tree's rows (nodes x heads of a KV head; more than 256 take several
+// tiles), unless trees of both sides of 128 rows meet: small ones would leave most
+// of an eight-wave workgroup idle, and a block takes it about as long with one
+// wave at work as with eight.  Those run tiles of 128, the large trees several
+// (12 trees of 5 to 61 nodes over 3K to 61K tokens: 303 us in tiles of 256, 246
+// in tiles of 128, 291 with a launch for each size of tree).
+struct DraftShape {
+  int32_t rows = 0, n_wg = 0, shared = 0;
+};
+DraftShape draft_shape(const sq_store *s, const int32_t *counts, int32_t batch) {
+  int32_t most = 0, least = INT32_MAX;
+  for (int b = 0; b < batch; ++b) {
+    most = std::max(most, counts[b] * s->G);
+    least = std::min(least, counts[b] * s->G);
+  }
+  DraftShape d;
+  d.rows = most <= 64 ? 64 : least > 128 ? 256 : 128;
+  if (s->kv8 && most <= 64) d.rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+  d.shared = most > d.rows;
+  const int per_cu = d.rows == 256 ? 1 : d.rows == 64 && s->D == 64 && !s->kv8 ? 3 : 2;
+  d.n_wg = std::min<int32_t>(s->cus * per_cu, sq::kDraftWgs);
+  return d;
 }
 
-// Deals the rows' blocks (nb[t] for every KV head of tile t) out to at most n_wg
-// workgroups in equal runs; kRowStart blocks stand for the start of a row.
+// The tiles of a draft, by the list of key blocks of one plan.
+struct DraftTile {
+  sq::DraftPiece as; // every field but KV head, blocks, slot and next
+  int64_t blocks;
+};
+// The tiles' blocks (for every KV head) dealt out to the workgroups in runs of
+// equal time: a block of a 128-row tile takes 10 with one wave at work, 13 with
+// four (16 in an 8-bit store), others about the same whatever the rows; the
+// start of a row, kRowStart blocks.
 constexpr int64_t kRowStart = 1;
 constexpr int64_t kMinRun = 3; // blocks a workgroup takes at least
-void draft_split(const std::vector<int64_t> &nb, int hkv, int32_t n_wg, sq::DraftSplit *out) {
-  int64_t total = 0;
-  for (int64_t b : nb) total += (b + kRowStart) * hkv;
-  const int64_t n = std::max<int64_t>(1, std::min<int64_t>(n_wg, total / kMinRun));
-  int32_t n_pieces = 0, slots = 0;
-  int64_t w = 0, at = 0; // the workgroup at flattened block `at`
+int32_t draft_split(const std::vector<DraftTile> &tiles, int hkv, int G, bool kv8, const DraftShape &shape,
+                    sq::DraftSplit *out) {
+  auto weight = [&](const DraftTile &t) -> int64_t {
+    const int waves = (t.as.n_nodes * G + 31) / 32;
+    return shape.rows == 128 ? 10 + (kv8 ? 2 : 1) * (waves - 1) : 10;
+  };
+  int64_t total = 0, blocks = 0;
+  for (const DraftTile &t : tiles) {
+    total += (t.blocks * weight(t) + kRowStart * 10) * hkv;
+    blocks += t.blocks * hkv;
+  }
+  // a workgroup leaves two partial tiles at most, and all together one each and
+  // one for every row
+  const int64_t most = (int64_t)sq::kMaxItems * sq::kRows / shape.rows;
+  const int64_t fit = std::max(most / 2, most - (int64_t)tiles.size() * hkv);
+  const int64_t n = std::max<int64_t>(1, std::min<int64_t>({shape.n_wg, fit, blocks / kMinRun}));
+  int32_t extra = (int32_t)n, slots = 0; // pieces behind the workgroups' first ones
+  int64_t w = 0, at = 0;                 // the workgroup at `at`, and its last piece
+  int32_t last = -1;
   auto end_of = [&](int64_t x) { return (x + 1) * total / n; };
-  out->piece0[0] = 0;
-  for (size_t t = 0; t < nb.size(); ++t)
+  for (int64_t i = 0; i < n; ++i) {
+    out->pieces[i] = sq::DraftPiece{};
+    out->pieces[i].next = -1; // (without blocks, unless it gets some below)
+  }
+  std::vector<int32_t> mine; // the row's pieces
+  for (size_t t = 0; t < tiles.size(); ++t) {
+    const int64_t wt = weight(tiles[t]), nb = tiles[t].blocks;
     for (int g = 0; g < hkv; ++g) {
-      const int32_t row = (int32_t)t * hkv + g, first = n_pieces;
-      int64_t b = 0;
-      const int64_t stop = at + nb[t] + kRowStart;
-      while (at < stop) {
-        while (end_of(w) <= at) out->piece0[++w] = n_pieces;
-        const int64_t upto = std::min(stop, end_of(w));
-        const int64_t e = std::min<int64_t>(nb[t], b + upto - at);
-        if (e > b) out->pieces[n_pieces++] = {row, (int32_t)b, (int32_t)e, -1};
-        b = e;
-        at = upto;
+      const int64_t stop = at + nb * wt + kRowStart * 10;
+      mine.clear();
+      for (int64_t b = 0; b < nb;) {
+        while (w + 1 < n && end_of(w) <= at) ++w, last = -1;
+        const int64_t x = end_of(w);
+        int64_t e = nb;
+        if (x < stop && w + 1 < n) e = std::min(nb, std::max(b, (x - (stop - nb * wt - kRowStart * 10) + wt / 2) / wt));
+        if (e > b) {
+          const int32_t p = last < 0 ? (int32_t)w : extra++;
+          if (last >= 0) out->pieces[last].next = p;
+          out->pieces[p] = tiles[t].as;
+          out->pieces[p].g = g;
+          out->pieces[p].b_lo = (int32_t)b;
+          out->pieces[p].b_hi = (int32_t)e;
+          out->pieces[p].slot = -1;
+          out->pieces[p].next = -1;
+          mine.push_back(p);
+          last = p;
+          b = e;
+        }
+        at = std::min(stop, x);
+        if (b < nb) ++w, last = -1;
       }
-      const int32_t cnt = n_pieces - first;
-      out->merge[row] = {slots, cnt > 1 ? cnt : 0};
+      at = stop;
+      const int32_t cnt = (int32_t)mine.size();
+      out->merge[t * hkv + g] = {slots * shape.rows, cnt > 1 ? cnt : 0};
       if (cnt > 1)
-        for (int32_t i = first; i < n_pieces; ++i) out->pieces[i].slot = slots++;
+        for (int32_t p : mine) out->pieces[p].slot = slots++ * shape.rows;
     }
-  while (w < n_wg) out->piece0[++w] = n_pieces;
+  }
+  out->n_used = (int32_t)n;
+  return extra;
 }
 
 // Depths of a tree's nodes; false for a parent that is no earlier node or -1.
@@ -2040,7 +2095,6 @@ sq_status open_tokens(sq_store *s, const sq_seq *seqs, const int32_t *counts, in
   if (batch < 1 || batch > SQ_MAX_BATCH) return fail(SQ_ERR_INVALID, "batch must be in [1, %d]", SQ_MAX_BATCH);
   if (s->open.kind == sq_store::Open::kDraft) return fail(SQ_ERR_INVALID, "a draft is open (accept it first)");
   int64_t need = 0, total = 0;
-  int32_t most = 0;
   std::vector<int32_t> depth;
   for (int b = 0; b < batch; ++b) {
     const Seq *q = s->get(seqs[b]);
@@ -2064,15 +2118,14 @@ sq_status open_tokens(sq_store *s, const sq_seq *seqs, const int32_t *counts, in
         return fail(SQ_ERR_INVALID, "a window over a sequence with masked slots (compact it first)");
     }
     need += want - (int64_t)q->pages.size();
-    most = std::max(most, (int32_t)n);
     total += n;
   }
   if (need > s->n_free)
     return fail(SQ_ERR_NO_PAGES, "%lld pages needed, %lld free", (long long)need, (long long)s->n_free);
-  int32_t rows = 0, n_wg = 0, per_tile = 0;
+  DraftShape shape;
   if (draft && s->device) {
-    draft_shape(s, most, &rows, &n_wg);
-    per_tile = rows / s->G;
+    shape = draft_shape(s, counts, batch);
+    const int32_t per_tile = shape.rows / s->G;
     int64_t n_rows = 0;
     for (int b = 0; b < batch; ++b) n_rows += (int64_t)((counts[b] + per_tile - 1) / per_tile) * s->cfg.num_kv_heads;
     if (n_rows > sq::kDraftRows)
@@ -2093,16 +2146,17 @@ sq_status open_tokens(sq_store *s, const sq_seq *seqs, const int32_t *counts, in
   op.kind = draft ? sq_store::Open::kDraft : sq_store::Open::kChunk;
   op.gen = s->gen;
   op.total = (int32_t)total;
-  op.rows = rows;
-  op.n_wg = n_wg;
+  op.rows = shape.rows;
+  op.n_wg = shape.n_wg;
+  op.shared = shape.shared;
   op.window = o.window;
   op.first = o.first;
   if (draft) op.parents.assign(parents, parents + total);
   sq::OpenArgs oa{};
   oa.plan.batch = batch;
   oa.plan.total = (int32_t)total;
-  std::vector<int64_t> nb[2];
-  int32_t tok0 = 0, n_tiles = 0;
+  std::vector<DraftTile> tiles[2]; // full plan, windowed plan
+  int32_t tok0 = 0;
   const int64_t tok_bytes = (int64_t)s->cfg.num_kv_heads * s->cfg.head_dim * 2 * s->elem_bytes();
   for (int b = 0; b < batch; ++b) {
     Seq &q = s->seqs[seqs[b]];
@@ -2161,29 +2215,33 @@ sq_status open_tokens(sq_store *s, const sq_seq *seqs, const int32_t *counts, in
         bl->depth[tok0 + i] = d;
       }
       int64_t lo_seq = L;
-      for (int32_t i0 = 0; i0 < n; i0 += per_tile, ++n_tiles) {
-        sq::DraftTile &t = bl->tiles[n_tiles];
-        t = sq::DraftTile{};
-        t.row = seqs[b];
-        t.base = (int32_t)base;
-        t.n = (int32_t)n;
-        t.n_pages = (int32_t)q.pages.size();
-        t.node0 = tok0 + i0;
-        t.n_nodes = std::min<int32_t>(per_tile, (int32_t)n - i0);
-        t.masked = q.n_masked > 0 ? 1 : 0;
-        int32_t lo_min = INT32_MAX;
-        for (int32_t i = 0; i < t.n_nodes; ++i) {
-          sq::DraftNode &nd = bl->nodes[t.node0 + i];
-          nd.tile = n_tiles;
+      const int32_t per_tile = shape.rows / s->G;
+      for (int32_t i0 = 0; i0 < n; i0 += per_tile) {
+        DraftTile t{};
+        t.as.row = seqs[b];
+        t.as.base = (int32_t)base;
+        t.as.n = (int32_t)n;
+        t.as.n_pages = (int32_t)q.pages.size();
+        t.as.node0 = tok0 + i0;
+        t.as.n_nodes = std::min<int32_t>(per_tile, (int32_t)n - i0);
+        t.as.masked = q.n_masked > 0 ? 1 : 0;
+        t.blocks = blocks;
+        int32_t lo_min = INT32_MAX, lo_max = 0;
+        for (int32_t i = 0; i < t.as.n_nodes; ++i) {
+          sq::DraftNode &nd = bl->nodes[t.as.node0 + i];
+          nd.tile = (int32_t)tiles[0].size();
+          nd.in_tile = i;
           lo_min = std::min(lo_min, nd.lo);
-          t.lo_max[1] = std::max(t.lo_max[1], nd.lo);
+          lo_max = std::max(lo_max, nd.lo);
         }
+        tiles[0].push_back(t);
         // windowed: the first tokens' blocks, then those from the window's start
         const int32_t from = lo_min / sq::kExtKeys;
-        t.nf[1] = std::min<int32_t>((int32_t)(((int64_t)o.first + sq::kExtKeys - 1) / sq::kExtKeys), from);
-        t.skip[1] = from - t.nf[1];
-        nb[0].push_back(blocks);
-        nb[1].push_back(blocks - t.skip[1]);
+        t.as.nf = std::min<int32_t>((int32_t)(((int64_t)o.first + sq::kExtKeys - 1) / sq::kExtKeys), from);
+        t.as.skip = from - t.as.nf;
+        t.as.lo_max = lo_max;
+        t.blocks = blocks - t.as.skip;
+        tiles[1].push_back(t);
         lo_seq = std::min<int64_t>(lo_seq, lo_min);
       }
       op.kv_bytes[0] += L * tok_bytes;
@@ -2203,14 +2261,13 @@ sq_status open_tokens(sq_store *s, const sq_seq *seqs, const int32_t *counts, in
   };
   part(bl->ids, op.n_units * sizeof(int32_t));
   if (draft) {
-    part(bl->tiles, n_tiles * sizeof(sq::DraftTile));
     part(bl->nodes, total * sizeof(sq::DraftNode));
     for (int w = 0; w < (o.window > 0 ? 2 : 1); ++w) {
       sq::DraftSplit &sp = bl->split[w];
-      draft_split(nb[w], s->cfg.num_kv_heads, n_wg, &sp);
-      part(sp.merge, (size_t)n_tiles * s->cfg.num_kv_heads * sizeof(sq::DraftMerge));
-      part(sp.piece0, (n_wg + 1) * sizeof(int32_t));
-      part(sp.pieces, sp.piece0[n_wg] * sizeof(sq::DraftPiece));
+      const int32_t n_pieces = draft_split(tiles[w], s->cfg.num_kv_heads, s->G, s->kv8, shape, &sp);
+      part(&sp.n_used, 16);
+      part(sp.merge, tiles[w].size() * s->cfg.num_kv_heads * sizeof(sq::DraftMerge));
+      part(sp.pieces, n_pieces * sizeof(sq::DraftPiece));
     }
   }
   oa.src = reinterpret_cast<const char *>(bl);
@@ -2412,6 +2469,7 @@ sq_status sq_draft_attn(sq_store *s, int32_t layer, const void *q, float *out, f
   a.first = o.window > 0 ? op.first : 0;
   a.rows = op.rows;
   a.n_wg = op.n_wg;
+  a.shared = op.shared;
   a.kv8 = s->kv8 ? 1 : 0;
   hipStream_t strm = static_cast<hipStream_t>(stream);
   s->last_stream = strm;
