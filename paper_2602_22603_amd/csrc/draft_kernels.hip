@@ -78,7 +78,7 @@ k_draft(DraftArgs a) {
     next = pc.next;
     if (b_lo >= b_hi) continue; // (a workgroup without work)
     const int L = base + n_draft;
-    const SeqPages pg{a.pt + (int64_t)pt_row * a.max_pages, n_pages, a.page_stride};
+    const SeqPages pg{a.pt + (int64_t)pt_row * a.max_pages, n_pages, kPage * D};
     const ext_sptr_t mask_row = (ext_sptr_t)(a.mask + (int64_t)pt_row * a.max_pages);
     // the block at place i of the row's list
     auto at = [&](int i) { return i < nf ? i : i + skip; };
@@ -160,11 +160,13 @@ k_draft(DraftArgs a) {
         const uint64_t cache = ~ones_from(base - k0); // keys of the cache
         const uint64_t early = ~ones_from(a.first - k0);
         const int off = base - k0; // place of node 0
+        int here = n; // (its own copy: nothing of this is to be held through the loop)
+        asm("" : "+v"(here));
 #pragma unroll
         for (int cg = 0; cg < 2; ++cg) {
           // a row past the nodes sees every key, so that it never has to look
           // for a first one
-          const int i = node_of(cg);
+          const int i = (32 * wave + 16 * cg + here) >> a.lg;
           const uint64_t anc = i < n_nodes ? s_anc[i] : ~0ull >> (64 - n_draft);
           uint64_t w = cache;
           if (plan && i < n_nodes) w &= ones_from(s_lo[i] - k0) | early;
@@ -212,13 +214,17 @@ k_draft(DraftArgs a) {
       __builtin_amdgcn_s_waitcnt(0);
     }
 
+    int tx = lane; // read again, so that no address below is held through the loop
+    asm("" : "+v"(tx));
+    const int n = tx & 15, kg = tx >> 4;
 #pragma unroll
     for (int cg = 0; cg < 2; ++cg) {
       float l = sum_xrow16(l_run[cg]);
       l = sum_xrow32(l);
-      if (node_of(cg) >= n_nodes) continue;
+      const int r0 = 32 * wave + 16 * cg + n, nd = r0 >> a.lg, head = (g << a.lg) + (r0 & ((1 << a.lg) - 1));
+      if (nd >= n_nodes) continue;
       if (slot >= 0) { // a part of the row's keys
-        const int64_t r = slot + 32 * wave + 16 * cg + n;
+        const int64_t r = slot + r0;
         if (kg == 0) {
           a.part_m[r] = m_run[cg];
           a.part_l[r] = l;
@@ -232,13 +238,13 @@ k_draft(DraftArgs a) {
       }
       float sc = 1.f;
       if (a.sinks) { // one more term of the sum, no value
-        const float sk_l2 = a.sinks[head_of(cg)] * a.sink_scale;
+        const float sk_l2 = a.sinks[head] * a.sink_scale;
         const float big = fmaxf(m_run[cg], sk_l2);
         sc = exp2_fast(m_run[cg] - big);
         l = fmaf(l, sc, exp2_fast(sk_l2 - big));
       }
       const float inv = sc / l * a.out_scale;
-      float *op = a.out + ((int64_t)(node0 + node_of(cg)) * a.hq + head_of(cg)) * D + 4 * kg;
+      float *op = a.out + ((int64_t)(node0 + nd) * a.hq + head) * D + 4 * kg;
 #pragma unroll
       for (int dt = 0; dt < NDT; ++dt)
         *reinterpret_cast<float4 *>(op + 16 * dt) = make_float4(acc[dt][cg][0] * inv, acc[dt][cg][1] * inv,
@@ -346,7 +352,7 @@ k_draft_stream(DraftArgs a) {
       id[1] = pt[min(p0 + 1, n_pages - 1)];
     };
     auto rsrc = [&](const char *head, int id, bool want) {
-      return page_rsrc(head + (int64_t)(want ? id : 0) * a.page_stride, want, kPageBytes);
+      return page_rsrc(head + (int64_t)(want ? id : 0) * kPageBytes, want, kPageBytes);
     };
     if (c_lo < c_hi) {
 #pragma unroll
@@ -392,11 +398,13 @@ k_draft_stream(DraftArgs a) {
         if (!in || k0 + 32 > base || (plan && k0 < lo_max && k0 + 32 > a.first) || keep != ~0u) {
           const uint64_t cache = ~ones_from(base - k0), early = ~ones_from(a.first - k0);
           const int off = base - k0; // place of node 0
+          int here = n, part = kg; // (their own copies: nothing of this is to be held through the loop)
+          asm("" : "+v"(here), "+v"(part));
 #pragma unroll
           for (int cg = 0; cg < CG; ++cg) {
             // a row past the nodes sees every key, so that it never has to look
             // for a first one
-            const int i = node_of(cg);
+            const int i = (WR * rg + 16 * cg + here) >> a.lg;
             const uint64_t anc = i < n_nodes ? s_anc[i] : ~0ull >> (64 - n_draft);
             uint64_t w = cache;
             if (plan && i < n_nodes) w &= ones_from(s_lo[i] - k0) | early;
@@ -406,7 +414,7 @@ k_draft_stream(DraftArgs a) {
             for (int h = 0; h < 2; ++h)
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (!((w32 >> (16 * h + 4 * kg + e)) & 1)) st[h][cg][e] = kNegInf;
+                if (!((w32 >> (16 * h + 4 * part + e)) & 1)) st[h][cg][e] = kNegInf;
           }
         }
         bf16x8_t phi[CG], plo[CG];
@@ -457,9 +465,11 @@ k_draft_stream(DraftArgs a) {
         for (int dt = 0; dt < NDT; ++dt) va[dt] = make_uint4(v0.v[dt].x, v0.v[dt].y, v1.v[dt].x, v1.v[dt].y);
         if (k0 + 32 > L) { // slots that hold no token may hold anything: keep 0 * v finite
           uint32_t m[4];
+          int part = kg;
+          asm("" : "+v"(part));
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const int k = k0 + 16 * (e >> 1) + 4 * kg + 2 * (e & 1);
+            const int k = k0 + 16 * (e >> 1) + 4 * part + 2 * (e & 1);
             m[e] = (k < L ? 0xffffu : 0u) | (k + 1 < L ? 0xffff0000u : 0u);
           }
 #pragma unroll
@@ -498,6 +508,9 @@ k_draft_stream(DraftArgs a) {
       *sc = *sc / l * a.out_scale;
       return a.out + ((int64_t)(node0 + (r >> a.lg)) * a.hq + (g << a.lg) + (r & ((1 << a.lg) - 1))) * D;
     };
+    int tx = tid; // read again, so that no address below is held through the loop
+    asm("" : "+v"(tx));
+    const int n = tx & 15, kg = (tx >> 4) & 3;
     if constexpr (KG > 1) {
 #pragma unroll
       for (int cg = 0; cg < CG; ++cg) {
@@ -513,7 +526,7 @@ k_draft_stream(DraftArgs a) {
               make_float4(acc[dt][cg][0], acc[dt][cg][1], acc[dt][cg][2], acc[dt][cg][3]);
       }
       __syncthreads();
-      for (int e = tid * 4; e < rows * D; e += 1024) {
+      for (int e = tx * 4; e < rows * D; e += 1024) {
         const int r = e / D, d = e % D, rw = r % WR, w0 = r / WR;
         float m = kNegInf, l = 0.f;
 #pragma unroll
