@@ -547,8 +547,8 @@ typedef struct sq_qk_opts {
  * int32 [n], >= 0; q_out bf16 [n][num_q_heads][D], k_out bf16
  * [n][num_kv_heads][D], packed, which may be q and k themselves where those
  * are packed.  opts NULL: a copy.  Needs no store; work is enqueued on
- * stream.  n = 0 does nothing.  SQ_ERR_INVALID: n < 0, head counts < 1, D
- * other than 64 or 128, q, k, q_out or k_out null or not 16-byte aligned,
+ * stream.  n = 0 does nothing.  SQ_ERR_INVALID: n outside [0, 2^24], head
+ * counts outside [1, 65536], D other than 64 or 128, q, k, q_out or k_out null or not 16-byte aligned,
  * positions null or not 4-byte aligned, a bad stride or option. */
 sq_status sq_qk_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                      const int32_t *positions, int32_t n, int32_t num_q_heads,

@@ -60,6 +60,7 @@ struct QkArgs {
   int32_t rot, interleaved;
   int32_t n, hq, hkv;
   int32_t its;                         // head iterations of one workgroup
+  int32_t blocks;                      // workgroups of one unit
   const OpenPlan *plan;
   const int32_t *ids;                  // page id of every unit
   uint16_t *k_pool, *v_pool;           // the layer's

@@ -2339,7 +2339,9 @@ sq_status sq_qk_rope(const void *q, int64_t q_stride, const void *k, int64_t k_s
                      int32_t num_kv_heads, int32_t head_dim, const sq_qk_opts *opts, void *q_out,
                      void *k_out, void *stream) {
   SQ_TRACE_CALL("sq_qk_rope", "n=%d q_heads=%d kv_heads=%d head_dim=%d", n, num_q_heads, num_kv_heads, head_dim);
-  if (n < 0 || num_q_heads < 1 || num_kv_heads < 1) return fail(SQ_ERR_INVALID, "n must be >= 0, head counts >= 1");
+  if (n < 0 || n > 1 << 24) return fail(SQ_ERR_INVALID, "n must be in [0, 2^24]");
+  if (num_q_heads < 1 || num_kv_heads < 1 || num_q_heads > 65536 || num_kv_heads > 65536)
+    return fail(SQ_ERR_INVALID, "head counts must be in [1, 65536]");
   if (head_dim != 64 && head_dim != 128) return fail(SQ_ERR_INVALID, "head_dim must be 64 or 128");
   sq::QkArgs a{};
   sq_status r = take_qk_opts(opts, head_dim, &a);

@@ -289,6 +289,27 @@ def test_qk_rope_refusals(sq):
     assert call(n=0, q=0) == sq.OK
 
 
+def test_qk_rope_refuses_sizes_past_its_grid(sq):
+    def call(n, hq, hkv):
+        return sq.lib().sq_qk_rope(16, 1 << 24, 32, 1 << 24, 4, n, hq, hkv, 128, None, 48, 64, None)
+
+    for bad in (((1 << 24) + 1, 1, 1), (2**31 - 1, 1, 1), (1, 65537, 1), (1, 1, 65537)):
+        assert call(*bad) == sq.ERR_INVALID, bad
+
+
+def test_trees_and_paths_are_integers(sq):
+    """Nodes that are no 32-bit integers are refused before the library sees them."""
+    s = _store(sq)
+    a = s.seq_create()
+    for bad in ([-1, 0.5], [-1, 1 << 31], [None], ["0"]):
+        _refused(s, sq.ERR_INVALID, s.draft_begin, [a], [bad])
+    s.draft_begin([a], [(-1, 0)])
+    _refused(s, sq.ERR_INVALID, s.draft_accept, [[0.0]])
+    s.draft_accept([(0, 1)])
+    assert s.seq_info(a)["length"] == 2
+    s.close()
+
+
 def test_first_tokens_of_a_window_are_checked(sq):
     """A metadata-only store checks step options before it opens the step."""
     import ctypes as C
