@@ -47,7 +47,6 @@ struct DraftMerge {
   int32_t row0, n;
 };
 
-constexpr int kDraftTiles = 4 * kMaxBatch;
 constexpr int kDraftRows = 4096; // (tile, KV head) rows
 constexpr int kDraftWgs = 1024;  // workgroups of a launch
 struct DraftSplit {
@@ -77,7 +76,6 @@ struct DraftArgs {
   float *out;        // fp32 [total][Hq][D]
   const int32_t *pt;
   const int32_t *mask;
-  int64_t page_stride;
   int64_t head_stride;
   int32_t max_pages;
   int32_t hq, hkv;

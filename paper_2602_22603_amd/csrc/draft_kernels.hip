@@ -43,6 +43,336 @@ struct SeqPages {
   int64_t page_stride;
 };
 
+// ---------------------------------------------------------------------------
+// The streaming form, for an 8-bit store and few rows: K and V go straight from
+// the pools to matrix-core operands in registers, with no LDS and no barrier
+// between a wave and its pages (the tiled form would pass the codes through
+// registers, LDS and a barrier: 4 nodes over 4 x 128K tokens 298 us, 211 so).  A
+// workgroup of 4 waves takes RG groups of 16 CG query rows against a piece's
+// keys; the 4 / RG waves of a row group take contiguous shares of the keys and
+// join their states in LDS at the end.  A step is a chunk of 32 keys (two
+// pages): S^T of page h (16 keys) lands with keys 4 kg + i in lane group kg,
+// which are slots (kg, 4 h + i) of the P^T operand, and the two pages' V^T
+// fragments side by side are the same slots of the V^T operand, so one
+// 16x16x32 product takes both pages.  PF chunks of K and V are in flight per
+// wave: chunk c + PF's K is loaded as soon as chunk c's scores are taken, its V
+// after the products.
+template <int WR> struct StreamLds {
+  float (*m)[WR], (*l)[WR]; // by wave: its rows' maxima and sums
+  uint64_t *anc;            // what the tile's nodes see
+  int32_t *lo;
+};
+// The waves' accumulators: rows of D + 4 floats,
+template <int D, int WR> struct PaddedRows {
+  float *base;
+  __device__ float *at(int wave, int row, int d) const { return base + (wave * WR + row) * (D + 4) + d; }
+};
+// or in four buffers of a tile, D floats a row, chunk c of row r at c ^ r.
+template <int D> struct SwizzledRows {
+  float *a0, *a1, *a2, *a3;
+  __device__ float *at(int wave, int row, int d) const {
+    float *p = wave == 0 ? a0 : wave == 1 ? a1 : wave == 2 ? a2 : a3;
+    return p + row * D + (((d >> 2) ^ row) & (D / 4 - 1)) * 4;
+  }
+};
+
+template <int D, int CG, int RG, class Rows>
+__device__ inline void stream_piece(const DraftArgs &a, const PieceRef &pc, const StreamLds<16 * CG> &lds,
+                                    const Rows &states) {
+  constexpr int NKC = D / 32, NDT = D / 16, KG = 4 / RG, PF = 2;
+  constexpr int WR = 16 * CG;        // rows of a wave
+  constexpr int kPageBytes = kPage * D;
+  constexpr bool NT = RG == 1;       // read by one wave: past the caches
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = lane & 15, kg = lane >> 4;
+  const int rg = wave % RG, kpart = wave / RG;
+  const int plan = a.windowed;
+  const int g = pc.g, base = pc.base, n_draft = pc.n, n_pages = pc.n_pages, node0 = pc.node0, n_nodes = pc.n_nodes;
+  const int masked = pc.masked, nf = pc.nf, skip = pc.skip, lo_max = pc.lo_max, b_lo = pc.b_lo, b_hi = pc.b_hi;
+  const int slot = pc.slot, pt_row = pc.row;
+  const int L = base + n_draft;
+  const ext_sptr_t pt = (ext_sptr_t)(a.pt + (int64_t)pt_row * a.max_pages);
+  const ext_sptr_t mask_row = (ext_sptr_t)(a.mask + (int64_t)pt_row * a.max_pages);
+  const char *khead = reinterpret_cast<const char *>(a.k) + (int64_t)g * a.head_stride;
+  const char *vhead = reinterpret_cast<const char *>(a.v) + (int64_t)g * a.head_stride;
+  const int koff = n * D + 16 * kg, voff = (16 * kg + n) * kPage;
+
+  __syncthreads(); // the piece before is done with the LDS
+  if (tid < n_nodes) {
+    lds.anc[tid] = a.blob->nodes[node0 + tid].anc[plan];
+    lds.lo[tid] = a.blob->nodes[node0 + tid].lo;
+  }
+  __syncthreads();
+  const int rows = n_nodes << a.lg;
+  auto node_of = [&](int cg) { return (WR * rg + 16 * cg + n) >> a.lg; }; // in the tile
+  auto head_of = [&](int cg) { return (g << a.lg) + ((WR * rg + 16 * cg + n) & ((1 << a.lg) - 1)); };
+  bf16x8_t qf[CG][NKC];
+#pragma unroll
+  for (int cg = 0; cg < CG; ++cg) {
+    const bool live = node_of(cg) < n_nodes;
+    const uint16_t *qp = a.q + ((int64_t)(node0 + node_of(cg)) * a.hq + head_of(cg)) * D;
+#pragma unroll
+    for (int kc = 0; kc < NKC; ++kc) {
+      const int c0 = 16 * kg + 64 * (kc >> 1) + 8 * (kc & 1); // the channels that the K fragments hold
+      qf[cg][kc] = __builtin_bit_cast(bf16x8_t, live ? *reinterpret_cast<const uint4 *>(qp + c0) : make_uint4(0, 0, 0, 0));
+    }
+  }
+  f32x4_t acc[NDT][CG];
+  float m_run[CG], l_run[CG];
+#pragma unroll
+  for (int cg = 0; cg < CG; ++cg) {
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt) acc[dt][cg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    m_run[cg] = kNegInf;
+    l_run[cg] = 0.f;
+  }
+
+  // this wave's chunks [c_lo, c_hi) of the piece's; the last block may end in
+  // its first chunk
+  auto key_of = [&](int c) {
+    const int i = b_lo + (c >> 1);
+    return (i < nf ? i : i + skip) * BK + 32 * (c & 1);
+  };
+  int total = 2 * (b_hi - b_lo);
+  if (key_of(total - 1) >= L) --total;
+  const int c_lo = WR * rg < rows ? total * kpart / KG : 0; // a row group without rows: nothing
+  const int c_hi = WR * rg < rows ? total * (kpart + 1) / KG : 0;
+  KFrag8<D> kf[PF][2];
+  VFrag8<D> vf[PF][2];
+  int nid[PF][2]; // page ids of the chunks to be loaded next
+  auto ids_of = [&](int c, int (&id)[2]) {
+    const int p0 = key_of(min(c, max(c_hi - 1, 0))) / kPage;
+    id[0] = pt[min(p0, n_pages - 1)];
+    id[1] = pt[min(p0 + 1, n_pages - 1)];
+  };
+  auto rsrc = [&](const char *head, int id, bool want) {
+    return page_rsrc(head + (int64_t)(want ? id : 0) * kPageBytes, want, kPageBytes);
+  };
+  if (c_lo < c_hi) {
+#pragma unroll
+    for (int u = 0; u < PF; ++u) {
+      ids_of(c_lo + u, nid[u]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        load_k<D, NT>(kf[u][h], rsrc(khead, nid[u][h], c_lo + u < c_hi), koff);
+        load_v<D, NT>(vf[u][h], rsrc(vhead, nid[u][h], c_lo + u < c_hi), voff);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < PF; ++u) ids_of(c_lo + PF + u, nid[u]);
+  }
+  const uint32_t m1l = minus_one(0), m1h = minus_one(1);
+  for (int c0 = c_lo; c0 < c_hi; c0 += PF) {
+#pragma unroll
+    for (int u = 0; u < PF; ++u) {
+      const int c = c0 + u;
+      const int k0 = key_of(c);
+      const bool in = c < c_hi; // a chunk past the share: zeros, and no key seen
+      f32x4_t st[2][CG];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const KFrag<D> kb = to_bf16(kf[u][h]);
+#pragma unroll
+        for (int cg = 0; cg < CG; ++cg) st[h][cg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kc = 0; kc < NKC; ++kc)
+#pragma unroll
+          for (int cg = 0; cg < CG; ++cg)
+            st[h][cg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kb.k[kc]), qf[cg][kc],
+                                                                st[h][cg], 0, 0, 0);
+      }
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load_k<D, NT>(kf[u][h], rsrc(khead, nid[u][h], c + PF < c_hi), koff);
+      // keep bits of the chunk's keys (deferred evictions)
+      uint32_t keep = ~0u;
+      if (masked) {
+        const int p0 = k0 / kPage, last = n_pages - 1;
+        keep = (uint32_t)mask_row[min(p0, last)] | (uint32_t)mask_row[min(p0 + 1, last)] << 16;
+      }
+      if (!in || k0 + 32 > base || (plan && k0 < lo_max && k0 + 32 > a.first) || keep != ~0u) {
+        const uint64_t cache = ~ones_from(base - k0), early = ~ones_from(a.first - k0);
+        const int off = base - k0; // place of node 0
+        int here = n, part = kg; // (their own copies: nothing of this is to be held through the loop)
+        asm("" : "+v"(here), "+v"(part));
+#pragma unroll
+        for (int cg = 0; cg < CG; ++cg) {
+          // a row past the nodes sees every key, so that it never has to look
+          // for a first one
+          const int i = (WR * rg + 16 * cg + here) >> a.lg;
+          const uint64_t anc = i < n_nodes ? lds.anc[i] : ~0ull >> (64 - n_draft);
+          uint64_t w = cache;
+          if (plan && i < n_nodes) w &= ones_from(lds.lo[i] - k0) | early;
+          if (off > -64 && off < 64) w |= off >= 0 ? anc << off : anc >> -off;
+          const uint32_t w32 = in ? (uint32_t)w & keep : 0u;
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!((w32 >> (16 * h + 4 * part + e)) & 1)) st[h][cg][e] = kNegInf;
+        }
+      }
+      bf16x8_t phi[CG], plo[CG];
+      float psum[CG];
+      for (bool raised = false;; raised = true) {
+        bool ok = true;
+#pragma unroll
+        for (int cg = 0; cg < CG; ++cg) {
+          const float nm = m_run[cg] == kNegInf ? 0.f : -m_run[cg];
+          uint32_t hi[4], lw[4];
+          psum[cg] = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float p0 = exp2_fast(fmaf(st[e >> 1][cg][2 * (e & 1)], a.scale_log2, nm));
+            const float p1 = exp2_fast(fmaf(st[e >> 1][cg][2 * (e & 1) + 1], a.scale_log2, nm));
+            hi[e] = pack_bf16(p0, p1);
+            lw[e] = pack_bf16(residue(hi[e], m1l, p0), residue(hi[e], m1h, p1));
+            psum[cg] += p0 + p1;
+          }
+          phi[cg] = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+          plo[cg] = __builtin_bit_cast(bf16x8_t, make_uint4(lw[0], lw[1], lw[2], lw[3]));
+          ok = ok && m_run[cg] != kNegInf && psum[cg] < kBig;
+        }
+        if (raised || __all(ok)) break;
+        // raise the references to this chunk's maxima and take the weights again
+        float alpha[CG];
+#pragma unroll
+        for (int cg = 0; cg < CG; ++cg) {
+          float mx = fmaxf(fmaxf(fmaxf(st[0][cg][0], st[0][cg][1]), fmaxf(st[0][cg][2], st[0][cg][3])),
+                           fmaxf(fmaxf(st[1][cg][0], st[1][cg][1]), fmaxf(st[1][cg][2], st[1][cg][3])));
+          mx = max_xrow16(mx);
+          mx = max_xrow32(mx) * a.scale_log2;
+          const float m_new = fmaxf(m_run[cg], mx);
+          alpha[cg] = m_new == m_run[cg] ? 1.f : exp2_fast(m_run[cg] - m_new); // 0 from -inf
+          m_run[cg] = m_new;
+          l_run[cg] *= alpha[cg];
+        }
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+          for (int cg = 0; cg < CG; ++cg) acc[dt][cg] *= alpha[cg];
+      }
+#pragma unroll
+      for (int cg = 0; cg < CG; ++cg) l_run[cg] += psum[cg];
+      const VFrag<D> v0 = to_bf16(vf[u][0]), v1 = to_bf16(vf[u][1]);
+      uint4 va[NDT];
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt) va[dt] = make_uint4(v0.v[dt].x, v0.v[dt].y, v1.v[dt].x, v1.v[dt].y);
+      if (k0 + 32 > L) { // slots that hold no token may hold anything: keep 0 * v finite
+        uint32_t m[4];
+        int part = kg;
+        asm("" : "+v"(part));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int k = k0 + 16 * (e >> 1) + 4 * part + 2 * (e & 1);
+          m[e] = (k < L ? 0xffffu : 0u) | (k + 1 < L ? 0xffff0000u : 0u);
+        }
+#pragma unroll
+        for (int dt = 0; dt < NDT; ++dt)
+          va[dt] = make_uint4(va[dt].x & m[0], va[dt].y & m[1], va[dt].z & m[2], va[dt].w & m[3]);
+      }
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int cg = 0; cg < CG; ++cg)
+          acc[dt][cg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va[dt]), phi[cg],
+                                                                acc[dt][cg], 0, 0, 0);
+#pragma unroll
+      for (int dt = 0; dt < NDT; ++dt)
+#pragma unroll
+        for (int cg = 0; cg < CG; ++cg)
+          acc[dt][cg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va[dt]), plo[cg],
+                                                                acc[dt][cg], 0, 0, 0);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) load_v<D, NT>(vf[u][h], rsrc(vhead, nid[u][h], c + PF < c_hi), voff);
+    }
+#pragma unroll
+    for (int u = 0; u < PF; ++u) ids_of(c0 + 2 * PF + u, nid[u]);
+  }
+
+  // The rows' states: of the row group's waves, joined (M = max m, out = sum
+  // 2^(m - M) acc), or this wave's own.
+  auto finish = [&](int r, float l, float m, float *sc) { // row r of the tile to the output
+    *sc = 1.f;
+    if (a.sinks) { // one more term of the sum, no value
+      const float sk_l2 = a.sinks[(g << a.lg) + (r & ((1 << a.lg) - 1))] * a.sink_scale;
+      const float big = fmaxf(m, sk_l2);
+      *sc = exp2_fast(m - big);
+      l = fmaf(l, *sc, exp2_fast(sk_l2 - big));
+    }
+    *sc = *sc / l * a.out_scale;
+    return a.out + ((int64_t)(node0 + (r >> a.lg)) * a.hq + (g << a.lg) + (r & ((1 << a.lg) - 1))) * D;
+  };
+  int tx = tid; // read again, so that no address below is held through the loop
+  asm("" : "+v"(tx));
+  const int en = tx & 15, ek = (tx >> 4) & 3;
+#pragma unroll
+  for (int cg = 0; cg < CG; ++cg) {
+    float l = sum_xrow16(l_run[cg]);
+    l = sum_xrow32(l);
+    if (ek == 0) {
+      lds.m[wave][16 * cg + en] = m_run[cg];
+      lds.l[wave][16 * cg + en] = l;
+    }
+#pragma unroll
+    for (int dt = 0; dt < NDT; ++dt)
+      *reinterpret_cast<float4 *>(states.at(wave, 16 * cg + en, 16 * dt + 4 * ek)) =
+          make_float4(acc[dt][cg][0], acc[dt][cg][1], acc[dt][cg][2], acc[dt][cg][3]);
+  }
+  __syncthreads();
+  for (int e = tx * 4; e < rows * D; e += 1024) {
+    const int r = e / D, d = e % D, rw = r % WR, w0 = r / WR;
+    float m = kNegInf, l = 0.f;
+#pragma unroll
+    for (int q = 0; q < KG; ++q) m = fmaxf(m, lds.m[w0 + RG * q][rw]);
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int q = 0; q < KG; ++q) {
+      const int w = w0 + RG * q;
+      const float sc = m == kNegInf ? 0.f : exp2_fast(lds.m[w][rw] - m);
+      l = fmaf(sc, lds.l[w][rw], l);
+      const float4 x = *reinterpret_cast<const float4 *>(states.at(w, rw, d));
+      o.x = fmaf(sc, x.x, o.x);
+      o.y = fmaf(sc, x.y, o.y);
+      o.z = fmaf(sc, x.z, o.z);
+      o.w = fmaf(sc, x.w, o.w);
+    }
+    if (slot >= 0) {
+      const int64_t pr = slot + r;
+      if (d == 0) {
+        a.part_m[pr] = m;
+        a.part_l[pr] = l;
+      }
+      *reinterpret_cast<float4 *>(a.part_acc + pr * D + d) = o;
+    } else {
+      float sc;
+      float *op = finish(r, l, m, &sc);
+      *reinterpret_cast<float4 *>(op + d) = make_float4(o.x * sc, o.y * sc, o.z * sc, o.w * sc);
+    }
+  }
+}
+
+template <int D, int CG, int RG>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void
+k_draft_stream(DraftArgs a) {
+  constexpr int WR = 16 * CG;
+  __shared__ float s_m[4][WR], s_l[4][WR];
+  __shared__ __attribute__((aligned(16))) float s_acc[4 * WR * (D + 4)];
+  __shared__ uint64_t s_anc[kMaxDraft];
+  __shared__ int32_t s_lo[kMaxDraft];
+  const DraftSplit &sp = a.blob->split[a.windowed];
+  int next = blockIdx.x;
+  if (next >= *(ext_sptr_t)&sp.n_used) return;
+  while (next >= 0) {
+    const PieceRef pc(sp.pieces[next]);
+    next = pc.next;
+    if (pc.b_lo >= pc.b_hi) continue; // (a workgroup without work)
+    stream_piece<D, CG, RG>(a, pc, StreamLds<WR>{s_m, s_l, s_anc, s_lo}, PaddedRows<D, WR>{s_acc});
+  }
+}
+
+// ---------------------------------------------------------------------------
 // NT: each key is read by one workgroup, past the caches (64 query rows over 4 x
 // 128K tokens: 372 us with temporal copies, 328 so).
 template <int D, int W, bool KV8, bool NT>
@@ -61,6 +391,8 @@ k_draft(DraftArgs a) {
   // registers it made the 256-row kernel spill)
   __shared__ uint64_t s_anc[kMaxDraft];
   __shared__ int32_t s_lo[kMaxDraft];
+  constexpr bool kSmall = KV8 && W == 4; // tiles of up to 64 rows in the streaming form
+  __shared__ float s_m[kSmall ? 4 : 1][32], s_l[kSmall ? 4 : 1][32];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -77,6 +409,16 @@ k_draft(DraftArgs a) {
     const int slot = pc.slot, pt_row = pc.row;
     next = pc.next;
     if (b_lo >= b_hi) continue; // (a workgroup without work)
+    if constexpr (kSmall) { // (a batch of mixed trees 237 us without, 186 with)
+      static_assert(Lt::K_ELEMS * 2 >= 32 * D * 4 && Lt::V_ELEMS * 2 >= 32 * D * 4, "a wave's accumulator in each");
+      const StreamLds<32> lds{s_m, s_l, s_anc, s_lo};
+      const SwizzledRows<D> states{reinterpret_cast<float *>(sk0), reinterpret_cast<float *>(sk1),
+                                   reinterpret_cast<float *>(sv0), reinterpret_cast<float *>(sv1)};
+      const int rows = n_nodes << a.lg;
+      if (rows <= 32) stream_piece<D, 2, 1>(a, pc, lds, states);
+      else if (rows <= 64) stream_piece<D, 2, 2>(a, pc, lds, states);
+      if (rows <= 64) continue;
+    }
     const int L = base + n_draft;
     const SeqPages pg{a.pt + (int64_t)pt_row * a.max_pages, n_pages, kPage * D};
     const ext_sptr_t mask_row = (ext_sptr_t)(a.mask + (int64_t)pt_row * a.max_pages);
@@ -249,336 +591,6 @@ k_draft(DraftArgs a) {
       for (int dt = 0; dt < NDT; ++dt)
         *reinterpret_cast<float4 *>(op + 16 * dt) = make_float4(acc[dt][cg][0] * inv, acc[dt][cg][1] * inv,
                                                                 acc[dt][cg][2] * inv, acc[dt][cg][3] * inv);
-    }
-  }
-}
-
-// ---------------------------------------------------------------------------
-// The streaming form, for an 8-bit store and few rows: K and V go straight from
-// the pools to matrix-core operands in registers, with no LDS and no barrier
-// between a wave and its pages (the tiled form would pass the codes through
-// registers, LDS and a barrier: 4 nodes over 4 x 128K tokens 298 us, 211 so).  A
-// workgroup of 4 waves takes RG groups of 16 CG query rows against a piece's
-// keys; the 4 / RG waves of a row group take contiguous shares of the keys and
-// join their states in LDS at the end.  A step is a chunk of 32 keys (two
-// pages): S^T of page h (16 keys) lands with keys 4 kg + i in lane group kg,
-// which are slots (kg, 4 h + i) of the P^T operand, and the two pages' V^T
-// fragments side by side are the same slots of the V^T operand, so one
-// 16x16x32 product takes both pages.  PF chunks of K and V are in flight per
-// wave: chunk c + PF's K is loaded as soon as chunk c's scores are taken, its V
-// after the products.
-template <int D, int CG, int RG>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2))) void
-k_draft_stream(DraftArgs a) {
-  constexpr int NKC = D / 32, NDT = D / 16, KG = 4 / RG, PF = 2;
-  constexpr int WR = 16 * CG;        // rows of a wave
-  constexpr int AP = D + 4;          // floats per row of a wave's accumulator in LDS
-  constexpr int kPageBytes = kPage * D;
-  constexpr bool NT = RG == 1;       // read by one wave: past the caches
-  __shared__ float s_m[KG > 1 ? 4 : 1][WR], s_l[KG > 1 ? 4 : 1][WR];
-  __shared__ __attribute__((aligned(16))) float s_acc[KG > 1 ? 4 : 1][KG > 1 ? WR * AP : 4];
-  __shared__ uint64_t s_anc[kMaxDraft];
-  __shared__ int32_t s_lo[kMaxDraft];
-
-  const int tid = threadIdx.x;
-  const int lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = lane & 15, kg = lane >> 4;
-  const int rg = wave % RG, kpart = wave / RG;
-  const int plan = a.windowed;
-  const DraftSplit &sp = a.blob->split[plan];
-  int next = blockIdx.x;
-  if (next >= *(ext_sptr_t)&sp.n_used) return;
-  for (bool again = false; next >= 0; again = true) {
-    const PieceRef pc(sp.pieces[next]);
-    const int g = pc.g, base = pc.base, n_draft = pc.n, n_pages = pc.n_pages, node0 = pc.node0, n_nodes = pc.n_nodes;
-    const int masked = pc.masked, nf = pc.nf, skip = pc.skip, lo_max = pc.lo_max, b_lo = pc.b_lo, b_hi = pc.b_hi;
-    const int slot = pc.slot, pt_row = pc.row;
-    next = pc.next;
-    if (b_lo >= b_hi) continue; // (a workgroup without work)
-    const int L = base + n_draft;
-    const ext_sptr_t pt = (ext_sptr_t)(a.pt + (int64_t)pt_row * a.max_pages);
-    const ext_sptr_t mask_row = (ext_sptr_t)(a.mask + (int64_t)pt_row * a.max_pages);
-    const char *khead = reinterpret_cast<const char *>(a.k) + (int64_t)g * a.head_stride;
-    const char *vhead = reinterpret_cast<const char *>(a.v) + (int64_t)g * a.head_stride;
-    const int koff = n * D + 16 * kg, voff = (16 * kg + n) * kPage;
-
-    if (again) __syncthreads(); // the piece before is done with the LDS
-    if (tid < n_nodes) {
-      s_anc[tid] = a.blob->nodes[node0 + tid].anc[plan];
-      s_lo[tid] = a.blob->nodes[node0 + tid].lo;
-    }
-    __syncthreads();
-    const int rows = n_nodes << a.lg;
-    auto node_of = [&](int cg) { return (WR * rg + 16 * cg + n) >> a.lg; }; // in the tile
-    auto head_of = [&](int cg) { return (g << a.lg) + ((WR * rg + 16 * cg + n) & ((1 << a.lg) - 1)); };
-    bf16x8_t qf[CG][NKC];
-#pragma unroll
-    for (int cg = 0; cg < CG; ++cg) {
-      const bool live = node_of(cg) < n_nodes;
-      const uint16_t *qp = a.q + ((int64_t)(node0 + node_of(cg)) * a.hq + head_of(cg)) * D;
-#pragma unroll
-      for (int kc = 0; kc < NKC; ++kc) {
-        const int c0 = 16 * kg + 64 * (kc >> 1) + 8 * (kc & 1); // the channels that the K fragments hold
-        qf[cg][kc] = __builtin_bit_cast(bf16x8_t, live ? *reinterpret_cast<const uint4 *>(qp + c0) : make_uint4(0, 0, 0, 0));
-      }
-    }
-    f32x4_t acc[NDT][CG];
-    float m_run[CG], l_run[CG];
-#pragma unroll
-    for (int cg = 0; cg < CG; ++cg) {
-#pragma unroll
-      for (int dt = 0; dt < NDT; ++dt) acc[dt][cg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-      m_run[cg] = kNegInf;
-      l_run[cg] = 0.f;
-    }
-
-    // this wave's chunks [c_lo, c_hi) of the piece's; the last block may end in
-    // its first chunk
-    auto key_of = [&](int c) {
-      const int i = b_lo + (c >> 1);
-      return (i < nf ? i : i + skip) * BK + 32 * (c & 1);
-    };
-    int total = 2 * (b_hi - b_lo);
-    if (key_of(total - 1) >= L) --total;
-    const int c_lo = WR * rg < rows ? total * kpart / KG : 0; // a row group without rows: nothing
-    const int c_hi = WR * rg < rows ? total * (kpart + 1) / KG : 0;
-    KFrag8<D> kf[PF][2];
-    VFrag8<D> vf[PF][2];
-    int nid[PF][2]; // page ids of the chunks to be loaded next
-    auto ids_of = [&](int c, int (&id)[2]) {
-      const int p0 = key_of(min(c, max(c_hi - 1, 0))) / kPage;
-      id[0] = pt[min(p0, n_pages - 1)];
-      id[1] = pt[min(p0 + 1, n_pages - 1)];
-    };
-    auto rsrc = [&](const char *head, int id, bool want) {
-      return page_rsrc(head + (int64_t)(want ? id : 0) * kPageBytes, want, kPageBytes);
-    };
-    if (c_lo < c_hi) {
-#pragma unroll
-      for (int u = 0; u < PF; ++u) {
-        ids_of(c_lo + u, nid[u]);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          load_k<D, NT>(kf[u][h], rsrc(khead, nid[u][h], c_lo + u < c_hi), koff);
-          load_v<D, NT>(vf[u][h], rsrc(vhead, nid[u][h], c_lo + u < c_hi), voff);
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < PF; ++u) ids_of(c_lo + PF + u, nid[u]);
-    }
-    const uint32_t m1l = minus_one(0), m1h = minus_one(1);
-    for (int c0 = c_lo; c0 < c_hi; c0 += PF) {
-#pragma unroll
-      for (int u = 0; u < PF; ++u) {
-        const int c = c0 + u;
-        const int k0 = key_of(c);
-        const bool in = c < c_hi; // a chunk past the share: zeros, and no key seen
-        f32x4_t st[2][CG];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const KFrag<D> kb = to_bf16(kf[u][h]);
-#pragma unroll
-          for (int cg = 0; cg < CG; ++cg) st[h][cg] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int kc = 0; kc < NKC; ++kc)
-#pragma unroll
-            for (int cg = 0; cg < CG; ++cg)
-              st[h][cg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, kb.k[kc]), qf[cg][kc],
-                                                                  st[h][cg], 0, 0, 0);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) load_k<D, NT>(kf[u][h], rsrc(khead, nid[u][h], c + PF < c_hi), koff);
-        // keep bits of the chunk's keys (deferred evictions)
-        uint32_t keep = ~0u;
-        if (masked) {
-          const int p0 = k0 / kPage, last = n_pages - 1;
-          keep = (uint32_t)mask_row[min(p0, last)] | (uint32_t)mask_row[min(p0 + 1, last)] << 16;
-        }
-        if (!in || k0 + 32 > base || (plan && k0 < lo_max && k0 + 32 > a.first) || keep != ~0u) {
-          const uint64_t cache = ~ones_from(base - k0), early = ~ones_from(a.first - k0);
-          const int off = base - k0; // place of node 0
-          int here = n, part = kg; // (their own copies: nothing of this is to be held through the loop)
-          asm("" : "+v"(here), "+v"(part));
-#pragma unroll
-          for (int cg = 0; cg < CG; ++cg) {
-            // a row past the nodes sees every key, so that it never has to look
-            // for a first one
-            const int i = (WR * rg + 16 * cg + here) >> a.lg;
-            const uint64_t anc = i < n_nodes ? s_anc[i] : ~0ull >> (64 - n_draft);
-            uint64_t w = cache;
-            if (plan && i < n_nodes) w &= ones_from(s_lo[i] - k0) | early;
-            if (off > -64 && off < 64) w |= off >= 0 ? anc << off : anc >> -off;
-            const uint32_t w32 = in ? (uint32_t)w & keep : 0u;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-              for (int e = 0; e < 4; ++e)
-                if (!((w32 >> (16 * h + 4 * part + e)) & 1)) st[h][cg][e] = kNegInf;
-          }
-        }
-        bf16x8_t phi[CG], plo[CG];
-        float psum[CG];
-        for (bool raised = false;; raised = true) {
-          bool ok = true;
-#pragma unroll
-          for (int cg = 0; cg < CG; ++cg) {
-            const float nm = m_run[cg] == kNegInf ? 0.f : -m_run[cg];
-            uint32_t hi[4], lw[4];
-            psum[cg] = 0.f;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float p0 = exp2_fast(fmaf(st[e >> 1][cg][2 * (e & 1)], a.scale_log2, nm));
-              const float p1 = exp2_fast(fmaf(st[e >> 1][cg][2 * (e & 1) + 1], a.scale_log2, nm));
-              hi[e] = pack_bf16(p0, p1);
-              lw[e] = pack_bf16(residue(hi[e], m1l, p0), residue(hi[e], m1h, p1));
-              psum[cg] += p0 + p1;
-            }
-            phi[cg] = __builtin_bit_cast(bf16x8_t, make_uint4(hi[0], hi[1], hi[2], hi[3]));
-            plo[cg] = __builtin_bit_cast(bf16x8_t, make_uint4(lw[0], lw[1], lw[2], lw[3]));
-            ok = ok && m_run[cg] != kNegInf && psum[cg] < kBig;
-          }
-          if (raised || __all(ok)) break;
-          // raise the references to this chunk's maxima and take the weights again
-          float alpha[CG];
-#pragma unroll
-          for (int cg = 0; cg < CG; ++cg) {
-            float mx = fmaxf(fmaxf(fmaxf(st[0][cg][0], st[0][cg][1]), fmaxf(st[0][cg][2], st[0][cg][3])),
-                             fmaxf(fmaxf(st[1][cg][0], st[1][cg][1]), fmaxf(st[1][cg][2], st[1][cg][3])));
-            mx = max_xrow16(mx);
-            mx = max_xrow32(mx) * a.scale_log2;
-            const float m_new = fmaxf(m_run[cg], mx);
-            alpha[cg] = m_new == m_run[cg] ? 1.f : exp2_fast(m_run[cg] - m_new); // 0 from -inf
-            m_run[cg] = m_new;
-            l_run[cg] *= alpha[cg];
-          }
-#pragma unroll
-          for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-            for (int cg = 0; cg < CG; ++cg) acc[dt][cg] *= alpha[cg];
-        }
-#pragma unroll
-        for (int cg = 0; cg < CG; ++cg) l_run[cg] += psum[cg];
-        const VFrag<D> v0 = to_bf16(vf[u][0]), v1 = to_bf16(vf[u][1]);
-        uint4 va[NDT];
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt) va[dt] = make_uint4(v0.v[dt].x, v0.v[dt].y, v1.v[dt].x, v1.v[dt].y);
-        if (k0 + 32 > L) { // slots that hold no token may hold anything: keep 0 * v finite
-          uint32_t m[4];
-          int part = kg;
-          asm("" : "+v"(part));
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int k = k0 + 16 * (e >> 1) + 4 * part + 2 * (e & 1);
-            m[e] = (k < L ? 0xffffu : 0u) | (k + 1 < L ? 0xffff0000u : 0u);
-          }
-#pragma unroll
-          for (int dt = 0; dt < NDT; ++dt)
-            va[dt] = make_uint4(va[dt].x & m[0], va[dt].y & m[1], va[dt].z & m[2], va[dt].w & m[3]);
-        }
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-          for (int cg = 0; cg < CG; ++cg)
-            acc[dt][cg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va[dt]), phi[cg],
-                                                                  acc[dt][cg], 0, 0, 0);
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt)
-#pragma unroll
-          for (int cg = 0; cg < CG; ++cg)
-            acc[dt][cg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, va[dt]), plo[cg],
-                                                                  acc[dt][cg], 0, 0, 0);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) load_v<D, NT>(vf[u][h], rsrc(vhead, nid[u][h], c + PF < c_hi), voff);
-      }
-#pragma unroll
-      for (int u = 0; u < PF; ++u) ids_of(c0 + 2 * PF + u, nid[u]);
-    }
-
-    // The rows' states: of the row group's waves, joined (M = max m, out = sum
-    // 2^(m - M) acc), or this wave's own.
-    auto finish = [&](int r, float l, float m, float *sc) { // row r of the tile to the output
-      *sc = 1.f;
-      if (a.sinks) { // one more term of the sum, no value
-        const float sk_l2 = a.sinks[(g << a.lg) + (r & ((1 << a.lg) - 1))] * a.sink_scale;
-        const float big = fmaxf(m, sk_l2);
-        *sc = exp2_fast(m - big);
-        l = fmaf(l, *sc, exp2_fast(sk_l2 - big));
-      }
-      *sc = *sc / l * a.out_scale;
-      return a.out + ((int64_t)(node0 + (r >> a.lg)) * a.hq + (g << a.lg) + (r & ((1 << a.lg) - 1))) * D;
-    };
-    int tx = tid; // read again, so that no address below is held through the loop
-    asm("" : "+v"(tx));
-    const int n = tx & 15, kg = (tx >> 4) & 3;
-    if constexpr (KG > 1) {
-#pragma unroll
-      for (int cg = 0; cg < CG; ++cg) {
-        float l = sum_xrow16(l_run[cg]);
-        l = sum_xrow32(l);
-        if (kg == 0) {
-          s_m[wave][16 * cg + n] = m_run[cg];
-          s_l[wave][16 * cg + n] = l;
-        }
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt)
-          *reinterpret_cast<float4 *>(&s_acc[wave][(16 * cg + n) * AP + 16 * dt + 4 * kg]) =
-              make_float4(acc[dt][cg][0], acc[dt][cg][1], acc[dt][cg][2], acc[dt][cg][3]);
-      }
-      __syncthreads();
-      for (int e = tx * 4; e < rows * D; e += 1024) {
-        const int r = e / D, d = e % D, rw = r % WR, w0 = r / WR;
-        float m = kNegInf, l = 0.f;
-#pragma unroll
-        for (int q = 0; q < KG; ++q) m = fmaxf(m, s_m[w0 + RG * q][rw]);
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int q = 0; q < KG; ++q) {
-          const int w = w0 + RG * q;
-          const float sc = m == kNegInf ? 0.f : exp2_fast(s_m[w][rw] - m);
-          l = fmaf(sc, s_l[w][rw], l);
-          const float4 x = *reinterpret_cast<const float4 *>(&s_acc[w][rw * AP + d]);
-          o.x = fmaf(sc, x.x, o.x);
-          o.y = fmaf(sc, x.y, o.y);
-          o.z = fmaf(sc, x.z, o.z);
-          o.w = fmaf(sc, x.w, o.w);
-        }
-        if (slot >= 0) {
-          const int64_t pr = slot + r;
-          if (d == 0) {
-            a.part_m[pr] = m;
-            a.part_l[pr] = l;
-          }
-          *reinterpret_cast<float4 *>(a.part_acc + pr * D + d) = o;
-        } else {
-          float sc;
-          float *op = finish(r, l, m, &sc);
-          *reinterpret_cast<float4 *>(op + d) = make_float4(o.x * sc, o.y * sc, o.z * sc, o.w * sc);
-        }
-      }
-    } else {
-#pragma unroll
-      for (int cg = 0; cg < CG; ++cg) {
-        float l = sum_xrow16(l_run[cg]);
-        l = sum_xrow32(l);
-        const int r = WR * rg + 16 * cg + n;
-        if (r >= rows) continue;
-        float sc = 1.f, *op;
-        if (slot >= 0) {
-          const int64_t pr = slot + r;
-          if (kg == 0) {
-            a.part_m[pr] = m_run[cg];
-            a.part_l[pr] = l;
-          }
-          op = a.part_acc + pr * D;
-        } else {
-          op = finish(r, l, m_run[cg], &sc);
-        }
-#pragma unroll
-        for (int dt = 0; dt < NDT; ++dt)
-          *reinterpret_cast<float4 *>(op + 16 * dt + 4 * kg) =
-              make_float4(acc[dt][cg][0] * sc, acc[dt][cg][1] * sc, acc[dt][cg][2] * sc, acc[dt][cg][3] * sc);
-      }
     }
   }
 }

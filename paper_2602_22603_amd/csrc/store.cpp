@@ -1986,8 +1986,9 @@ namespace {
 // tiles), unless trees of both sides of 128 rows meet: small ones would leave most
 // of an eight-wave workgroup idle, and a block takes it about as long with one
 // wave at work as with eight.  Those run tiles of 128, the large trees several
-// (12 trees of 5 to 61 nodes over 3K to 61K tokens: 303 us in tiles of 256, 246
-// in tiles of 128, 291 with a launch for each size of tree).
+// (12 trees of 5 to 61 nodes over 3K to 61K tokens of an 8-bit store: 303 us in
+// tiles of 256, 246 in tiles of 128, 291 with a launch for each size of tree; 186
+// now that an 8-bit store's tiles of up to 64 rows are streamed inside that launch).
 struct DraftShape {
   int32_t rows = 0, n_wg = 0, shared = 0;
 };
@@ -2013,15 +2014,20 @@ struct DraftTile {
 };
 // The tiles' blocks (for every KV head) dealt out to the workgroups in runs of
 // equal time: a block of a 128-row tile takes 10 with one wave at work, 13 with
-// four (16 in an 8-bit store), others about the same whatever the rows; the
-// start of a row, kRowStart blocks.
+// four; in an 8-bit store 6 and 9 where it is streamed (up to 32 and 64 rows), 14
+// and 16 where not; others about the same whatever the rows; the start of a row,
+// kRowStart blocks.
 constexpr int64_t kRowStart = 1;
-constexpr int64_t kMinRun = 3; // blocks a workgroup takes at least
+// A workgroup takes three blocks at least, one (of a 256-row tile two) while there
+// is a CU for each: 12 nodes over 1000 tokens 20.3 us with three, 15.7 with one;
+// past a workgroup a CU, 30 over 4 x 1500 tokens 27 with three, 33 with one.
+constexpr int64_t kMinRun = 3;
 int32_t draft_split(const std::vector<DraftTile> &tiles, int hkv, int G, bool kv8, const DraftShape &shape,
-                    sq::DraftSplit *out) {
+                    int cus, sq::DraftSplit *out) {
   auto weight = [&](const DraftTile &t) -> int64_t {
     const int waves = (t.as.n_nodes * G + 31) / 32;
-    return shape.rows == 128 ? 10 + (kv8 ? 2 : 1) * (waves - 1) : 10;
+    static constexpr int w8[4] = {6, 9, 14, 16};
+    return shape.rows != 128 ? 10 : kv8 ? w8[waves - 1] : 10 + waves - 1;
   };
   int64_t total = 0, blocks = 0;
   for (const DraftTile &t : tiles) {
@@ -2032,7 +2038,8 @@ int32_t draft_split(const std::vector<DraftTile> &tiles, int hkv, int G, bool kv
   // one for every row
   const int64_t most = (int64_t)sq::kMaxItems * sq::kRows / shape.rows;
   const int64_t fit = std::max(most / 2, most - (int64_t)tiles.size() * hkv);
-  const int64_t n = std::max<int64_t>(1, std::min<int64_t>({shape.n_wg, fit, blocks / kMinRun}));
+  const int64_t runs = std::max(blocks / kMinRun, std::min<int64_t>(cus, blocks / (shape.rows == 256 ? 2 : 1)));
+  const int64_t n = std::max<int64_t>(1, std::min<int64_t>({shape.n_wg, fit, runs}));
   int32_t extra = (int32_t)n, slots = 0; // pieces behind the workgroups' first ones
   int64_t w = 0, at = 0;                 // the workgroup at `at`, and its last piece
   int32_t last = -1;
@@ -2264,7 +2271,7 @@ sq_status open_tokens(sq_store *s, const sq_seq *seqs, const int32_t *counts, in
     part(bl->nodes, total * sizeof(sq::DraftNode));
     for (int w = 0; w < (o.window > 0 ? 2 : 1); ++w) {
       sq::DraftSplit &sp = bl->split[w];
-      const int32_t n_pieces = draft_split(tiles[w], s->cfg.num_kv_heads, s->G, s->kv8, shape, &sp);
+      const int32_t n_pieces = draft_split(tiles[w], s->cfg.num_kv_heads, s->G, s->kv8, shape, s->cus, &sp);
       part(&sp.n_used, 16);
       part(sp.merge, tiles[w].size() * s->cfg.num_kv_heads * sizeof(sq::DraftMerge));
       part(sp.pieces, n_pieces * sizeof(sq::DraftPiece));
@@ -2452,7 +2459,6 @@ sq_status sq_draft_attn(sq_store *s, int32_t layer, const void *q, float *out, f
   a.out = out;
   a.pt = s->pt_dev;
   a.mask = s->mask_dev;
-  a.page_stride = s->pools.page_stride;
   a.head_stride = s->pools.head_stride;
   a.max_pages = s->cfg.max_pages_per_seq;
   a.hq = s->cfg.num_q_heads;
