@@ -562,7 +562,7 @@ sq_status sq_qk_rope(const void *q, int64_t q_stride, const void *k, int64_t k_s
  * sq_reserve errors change nothing.  SQ_ERR_INVALID: batch outside [1,
  * SQ_MAX_BATCH], a repeated sequence, a count < 1, more than SQ_MAX_RESERVE
  * tokens, a sequence past its page-list capacity, positions past int32, an
- * open draft; SQ_ERR_NO_PAGES.  A metadata-only store changes its metadata. */
+ * open draft, a stream in capture; SQ_ERR_NO_PAGES.  A metadata-only store changes its metadata. */
 #define SQ_MAX_RESERVE 262144
 sq_status sq_reserve(sq_store *store, const sq_seq *seqs, const int32_t *counts, int32_t batch,
                      void *stream);
@@ -585,7 +585,8 @@ sq_status sq_qkv_store(sq_store *store, int32_t layer, const void *q, int64_t q_
  * tail): their pages lose a reference, and the next appended token gets the
  * position of the first dropped one.  A last page that ends up part full
  * while another branch holds it too is first copied to a new page.
- * SQ_ERR_INVALID: length outside [0, length of seq], an open draft on seq;
+ * SQ_ERR_INVALID: length outside [0, length of seq], an open draft on seq, a
+ * stream in capture;
  * SQ_ERR_SPAN: a registered span ends past length; SQ_ERR_NO_PAGES: no page
  * for that copy. */
 sq_status sq_truncate(sq_store *store, sq_seq seq, int64_t length, void *stream);
@@ -612,7 +613,8 @@ sq_status sq_truncate(sq_store *store, sq_seq seq, int64_t length, void *stream)
  * SQ_ERR_INVALID: batch outside [1, SQ_MAX_BATCH], a repeated sequence, a
  * count outside [1, SQ_MAX_DRAFT], a bad parent, an open draft, a sequence
  * past its page-list capacity, a window over masked slots, more than 4096
- * (sequence, KV head) rows of work, bad options; SQ_ERR_NO_PAGES.  Errors
+ * (sequence, KV head) rows of work, bad options, a stream in capture;
+ * SQ_ERR_NO_PAGES.  Errors
  * change nothing. */
 sq_status sq_draft_begin(sq_store *store, const sq_seq *seqs, const int32_t *counts, int32_t batch,
                          const int32_t *parents, const sq_attn_opts *opts, void *stream);
@@ -638,7 +640,7 @@ sq_status sq_draft_attn(sq_store *store, int32_t layer, const void *q, float *ou
  * Their K and V of every layer and their positions move to the slots right
  * behind the sequence's tokens; the other nodes' pages are freed.
  * SQ_ERR_INVALID: no open draft, a count outside [0, the begin's], nodes that
- * are no such path (the draft stays open). */
+ * are no such path, a stream in capture (the draft stays open). */
 sq_status sq_draft_accept(sq_store *store, const int32_t *counts, const int32_t *nodes,
                           void *stream);
 

@@ -89,7 +89,7 @@ __device__ inline void stream_piece(const DraftArgs &a, const PieceRef &pc, cons
   const int n = lane & 15, kg = lane >> 4;
   const int rg = wave % RG, kpart = wave / RG;
   const int plan = a.windowed;
-  const int g = pc.g, base = pc.base, n_draft = pc.n, n_pages = pc.n_pages, node0 = pc.node0, n_nodes = pc.n_nodes;
+  const int g = pc.g, base = pc.base, n_draft = pc.n, n_pages = pc.n_pages, node0 = pc.node0, n_nodes = min(pc.n_nodes, a.total - pc.node0);
   const int masked = pc.masked, nf = pc.nf, skip = pc.skip, lo_max = pc.lo_max, b_lo = pc.b_lo, b_hi = pc.b_hi;
   const int slot = pc.slot, pt_row = pc.row;
   const int L = base + n_draft;
@@ -404,7 +404,7 @@ k_draft(DraftArgs a) {
   if (next >= *(ext_sptr_t)&sp.n_used) return;
   while (next >= 0) {
     const PieceRef pc(sp.pieces[next]);
-    const int g = pc.g, base = pc.base, n_draft = pc.n, n_pages = pc.n_pages, node0 = pc.node0, n_nodes = pc.n_nodes;
+    const int g = pc.g, base = pc.base, n_draft = pc.n, n_pages = pc.n_pages, node0 = pc.node0, n_nodes = min(pc.n_nodes, a.total - pc.node0);
     const int masked = pc.masked, nf = pc.nf, skip = pc.skip, lo_max = pc.lo_max, b_lo = pc.b_lo, b_hi = pc.b_hi;
     const int slot = pc.slot, pt_row = pc.row;
     next = pc.next;

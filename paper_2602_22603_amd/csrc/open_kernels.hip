@@ -155,7 +155,7 @@ __global__ __launch_bounds__(256) void k_qk(QkArgs a) {
     if (page < 0) return; // (the whole workgroup)
     const int base = pl->base[e], first = (base / P + u - pl->unit0[e]) * P - base; // entry token of slot 0
     s0 = max(0, -first);
-    s1 = min(P, pl->n[e] - first);
+    s1 = min(P, min(pl->n[e], a.n - pl->tok0[e]) - first);
     t = pl->tok0[e] + first + row;
   } else {
     s1 = min(P, a.n - u * P);

@@ -2086,6 +2086,18 @@ int32_t draft_split(const std::vector<DraftTile> &tiles, int hkv, int G, bool kv
   return extra;
 }
 
+bool capturing(hipStream_t strm) {
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  (void)hipStreamIsCapturing(strm, &cap);
+  return cap != hipStreamCaptureStatusNone;
+}
+// Calls that change which slots hold what run once, not with every replay.
+sq_status no_capture(const sq_store *s, void *stream) {
+  if (s->device && capturing(static_cast<hipStream_t>(stream)))
+    return fail(SQ_ERR_INVALID, "not in a stream capture");
+  return SQ_OK;
+}
+
 // Depths of a tree's nodes; false for a parent that is no earlier node or -1.
 bool tree_depths(const int32_t *parents, int32_t n, int32_t *depth) {
   for (int32_t i = 0; i < n; ++i) {
@@ -2101,6 +2113,8 @@ sq_status open_tokens(sq_store *s, const sq_seq *seqs, const int32_t *counts, in
   const bool draft = parents != nullptr;
   if (batch < 1 || batch > SQ_MAX_BATCH) return fail(SQ_ERR_INVALID, "batch must be in [1, %d]", SQ_MAX_BATCH);
   if (s->open.kind == sq_store::Open::kDraft) return fail(SQ_ERR_INVALID, "a draft is open (accept it first)");
+  sq_status r = no_capture(s, stream);
+  if (r != SQ_OK) return r;
   int64_t need = 0, total = 0;
   std::vector<int32_t> depth;
   for (int b = 0; b < batch; ++b) {
@@ -2327,12 +2341,6 @@ sq_status check_rows(const void *p, int64_t stride, int64_t heads, int D, const 
   return SQ_OK;
 }
 
-bool capturing(hipStream_t strm) {
-  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
-  (void)hipStreamIsCapturing(strm, &cap);
-  return cap != hipStreamCaptureStatusNone;
-}
-
 // The open draft, if there is one.
 sq_status open_draft(sq_store *s) {
   if (s->open.kind != sq_store::Open::kDraft) return fail(SQ_ERR_INVALID, "no draft is open");
@@ -2516,7 +2524,7 @@ sq_status sq_draft_accept(sq_store *s, const int32_t *counts, const int32_t *nod
   SQ_TRACE_CALL("sq_draft_accept", "store=%p batch=%d", (void *)s, s ? (int)s->open.seqs.size() : 0);
   if (!s || !counts) return fail(SQ_ERR_INVALID, "null argument");
   sq_status r = open_draft(s);
-  if (r != SQ_OK) return r;
+  if (r != SQ_OK || (r = no_capture(s, stream)) != SQ_OK) return r;
   sq_store::Open &op = s->open;
   const int batch = (int)op.seqs.size();
   sq::AcceptArgs a{};
@@ -2571,7 +2579,7 @@ sq_status sq_truncate(sq_store *s, sq_seq h, int64_t length, void *stream) {
   Seq *q = s->get(h);
   if (!q) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", h);
   sq_status r = no_draft(*q, h);
-  if (r != SQ_OK) return r;
+  if (r != SQ_OK || (r = no_capture(s, stream)) != SQ_OK) return r;
   if (length < 0 || length > q->length)
     return fail(SQ_ERR_INVALID, "length %lld outside [0, %lld]", (long long)length, (long long)q->length);
   for (auto &kv : q->spans)

@@ -287,7 +287,11 @@ def _packed(t, shape, dtype, dev, what):
 def _current(dev):
     """The library launches on the current device, where its buffers must be."""
     import torch
-    if dev.type != "cuda" or dev.index not in (None, torch.cuda.current_device()):
+    try:  # (as for the stream above)
+        at = torch._C._cuda_getDevice()
+    except AttributeError:
+        at = torch.cuda.current_device()
+    if dev.index != at:  # None on a CPU
         raise SqError(ERR_INVALID, f"tensors on {dev}: make it the current device")
 
 
@@ -723,6 +727,8 @@ class Store:
         paths = [list(p) for p in paths]
         if len(paths) != getattr(self, "_draft_seqs", 0):
             raise SqError(ERR_INVALID, "one path for each sequence of the open draft")
+        if not self.metadata_only:
+            _current(self.k_pool.device)
         st = C.c_void_p(0) if self.metadata_only else _stream(stream)
         _check(lib().sq_draft_accept(self._handle, _i32_array([len(p) for p in paths]),
                                      _i32_joined(paths), st))

@@ -425,6 +425,61 @@ def test_captured_layer_replays_for_later_drafts(sq):
         assert torch.equal(out, want) and torch.equal(outw, wantw) and out.abs().sum() > 0
 
 
+def test_a_capture_takes_no_call_that_moves_slots(sq):
+    """reserve, draft_begin, draft_accept and truncate are refused in a capture,
+    changing nothing and leaving the capture whole."""
+    import torch
+    b = Batch(sq, 8, 2, 64, [50], [5], seed=1)
+    s, h = b.s, b.seqs[0]
+    x = torch.zeros(4, device="cuda")
+    for call in (lambda: s.reserve([h], [3]), lambda: s.draft_begin([h], [[-1]]), lambda: s.truncate(h, 20),
+                 lambda: s.draft_accept([[0]])):
+        if call.__code__.co_names[0] == "draft_accept":
+            b.begin()
+        before, graph = s.seq_info(h), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            x.add_(1)
+            with pytest.raises(sq.SqError):
+                call()
+        assert s.seq_info(h) == before
+        graph.replay()
+    torch.cuda.synchronize()
+    assert x.tolist() == [4.0] * 4
+    b.check()
+    s.draft_accept([[0]])
+    s.truncate(h, 20)
+    assert s.seq_info(h)["length"] == 20
+
+
+@pytest.mark.parametrize("kv8", [False, True])
+def test_a_replay_for_a_larger_draft_stays_in_its_buffers(sq, kv8):
+    """A capture is for drafts of its own counts.  Replayed with a larger one
+    open, it writes nothing behind the rows it was captured with."""
+    import torch
+    b = Batch(sq, 16, 4, 128, [700], [64], kv8, seed=9)
+    s, h = b.s, b.seqs[0]
+    q, kn, vn = (torch.zeros(64, n, 128, device="cuda", dtype=torch.bfloat16) for n in (16, 4, 4))
+    stored, out = torch.zeros_like(q), torch.zeros(64, 16, 128, device="cuda")
+    for n in (5, 12, 33):
+        s.draft_begin([h], [b.trees[0][:n]])
+        s.qkv_store(0, q[:n], kn[:n], vn[:n], q_out=stored[:n])
+        s.draft_attn(0, stored[:n], out=out[:n])
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            s.qkv_store(0, q[:n], kn[:n], vn[:n], q_out=stored[:n])
+            s.draft_attn(0, stored[:n], out=out[:n])
+        s.draft_accept([[]])
+        stored.fill_(7), out.fill_(7)
+        s.draft_begin([h], b.trees)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert (stored[n:] == 7).all() and (out[n:] == 7).all()
+        s.draft_accept([[]])
+    b.begin()
+    b.check()
+
+
 def test_same_inputs_give_the_same_bits_on_any_stream(sq):
     import torch
     b = Batch(sq, 32, 8, 128, [5000, 3000], [30, 64], seed=6)
