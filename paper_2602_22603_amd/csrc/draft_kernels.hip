@@ -596,32 +596,42 @@ k_draft(DraftArgs a) {
 }
 
 // The rows whose keys were split: M = max m_s, out = sum 2^(m_s - M) acc_s / sum
-// 2^(m_s - M) l_s.  A workgroup of NW waves takes one (node, head), each wave a
-// share of its partial slots, lanes over channels.
-template <int D, int NW>
-__global__ __launch_bounds__(64 * NW) void k_draft_merge(DraftArgs a) {
-  constexpr int DPT = D / 64;
-  constexpr int U = 8;
-  __shared__ float s_m[NW], s_l[NW], s_acc[NW][D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int i = blockIdx.x / a.hq, h = blockIdx.x % a.hq;
+// 2^(m_s - M) l_s.  D / 4 lanes take a (node, head)'s slots, four channels each, a
+// workgroup 1024 / D of them; or, SHARED, all of a workgroup's lane groups take
+// shares of one row's slots, for few rows whose keys were split over the chip.
+// Bound by the partial rows it reads (64 nodes over 60547 tokens: 34 MB, 7.2 us)
+// and, below some MB, by a chain of four loads (3 us).  With a wave to a row, 13760
+// rows of 64 channels took 6.9 us, 5.8 so.
+template <int D, bool SHARED>
+__global__ __launch_bounds__(256) void k_draft_merge(DraftArgs a) {
+  constexpr int L = D / 4, GROUPS = 256 / L, SH = SHARED ? GROUPS : 1;
+  constexpr int U = SHARED ? 4 : 8;
+  __shared__ float s_m[GROUPS], s_l[GROUPS];
+  __shared__ __attribute__((aligned(16))) float s_acc[SHARED ? GROUPS : 1][D];
+  const int lane = threadIdx.x % L, group = threadIdx.x / L, share = SHARED ? group : 0;
+  const int r = SHARED ? blockIdx.x : blockIdx.x * GROUPS + group;
+  const bool live = r < a.total * a.hq;
+  const int i = live ? r / a.hq : 0, h = live ? r % a.hq : 0;
   const int tile = a.blob->nodes[i].tile, in_tile = a.blob->nodes[i].in_tile;
   const int g = h >> a.lg;
   const DraftMerge mr = a.blob->split[a.windowed].merge[tile * a.hkv + g];
-  if (mr.n == 0) return;
+  if (!live || mr.n == 0) return; // (SHARED: the whole workgroup)
   const int col = (in_tile << a.lg) + (h & ((1 << a.lg) - 1));
-  float big = kNegInf, den = 0.f, num[DPT];
-#pragma unroll
-  for (int q = 0; q < DPT; ++q) num[q] = 0.f;
-  for (int s0 = wave * U; s0 < mr.n; s0 += NW * U) {
-    float x[U][DPT], m[U], l[U];
+  float big = kNegInf, den = 0.f;
+  float4 num = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto scale = [](float4 x, float w) { return make_float4(x.x * w, x.y * w, x.z * w, x.w * w); };
+  auto add = [](float4 s, float4 x, float w) {
+    return make_float4(fmaf(w, x.x, s.x), fmaf(w, x.y, s.y), fmaf(w, x.z, s.z), fmaf(w, x.w, s.w));
+  };
+  for (int s0 = share * U; s0 < mr.n; s0 += SH * U) {
+    float4 x[U];
+    float m[U], l[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t r = mr.row0 + (int64_t)min(s0 + u, mr.n - 1) * a.rows + col;
-      m[u] = s0 + u < mr.n ? a.part_m[r] : kNegInf;
-      l[u] = a.part_l[r];
-#pragma unroll
-      for (int q = 0; q < DPT; ++q) x[u][q] = a.part_acc[r * D + lane * DPT + q];
+      const int64_t at = mr.row0 + (int64_t)min(s0 + u, mr.n - 1) * a.rows + col;
+      m[u] = s0 + u < mr.n ? a.part_m[at] : kNegInf;
+      l[u] = a.part_l[at];
+      x[u] = reinterpret_cast<const float4 *>(a.part_acc + at * D)[lane];
     }
     float top = big;
 #pragma unroll
@@ -629,40 +639,35 @@ __global__ __launch_bounds__(64 * NW) void k_draft_merge(DraftArgs a) {
     if (top == kNegInf) continue;
     const float sc = exp2_fast(big - top);
     den *= sc;
-#pragma unroll
-    for (int q = 0; q < DPT; ++q) num[q] *= sc;
+    num = scale(num, sc);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const float w = exp2_fast(m[u] - top);
       den = fmaf(w, l[u], den);
-#pragma unroll
-      for (int q = 0; q < DPT; ++q) num[q] = fmaf(w, x[u][q], num[q]);
+      num = add(num, x[u], w);
     }
     big = top;
   }
-  if (NW > 1) {
+  if constexpr (SHARED) {
     if (lane == 0) {
-      s_m[wave] = big;
-      s_l[wave] = den;
+      s_m[group] = big;
+      s_l[group] = den;
     }
-#pragma unroll
-    for (int q = 0; q < DPT; ++q) s_acc[wave][lane * DPT + q] = num[q];
+    reinterpret_cast<float4 *>(s_acc[group])[lane] = num;
     __syncthreads();
-    if (wave != 0) return;
+    if (group != 0) return;
     float top = kNegInf;
 #pragma unroll
-    for (int w = 0; w < NW; ++w) top = fmaxf(top, s_m[w]);
+    for (int w = 0; w < GROUPS; ++w) top = fmaxf(top, s_m[w]);
     den = 0.f;
-#pragma unroll
-    for (int q = 0; q < DPT; ++q) num[q] = 0.f;
+    num = make_float4(0.f, 0.f, 0.f, 0.f);
     big = top;
     if (top != kNegInf) {
 #pragma unroll
-      for (int w = 0; w < NW; ++w) {
+      for (int w = 0; w < GROUPS; ++w) {
         const float sc = exp2_fast(s_m[w] - top);
         den = fmaf(sc, s_l[w], den);
-#pragma unroll
-        for (int q = 0; q < DPT; ++q) num[q] = fmaf(sc, s_acc[w][lane * DPT + q], num[q]);
+        num = add(num, reinterpret_cast<const float4 *>(s_acc[w])[lane], sc);
       }
     }
   }
@@ -673,9 +678,7 @@ __global__ __launch_bounds__(64 * NW) void k_draft_merge(DraftArgs a) {
     den = fmaf(den, sc, exp2_fast(sink - top));
   }
   sc = sc / den * a.out_scale; // (a node sees itself, so there is always a term)
-  float *op = a.out + ((int64_t)i * a.hq + h) * D + lane * DPT;
-#pragma unroll
-  for (int q = 0; q < DPT; ++q) op[q] = num[q] * sc;
+  reinterpret_cast<float4 *>(a.out + ((int64_t)i * a.hq + h) * D)[lane] = scale(num, sc);
 }
 
 template <int D, int W> hipError_t tile_dispatch(const DraftArgs &a, hipStream_t s) {
@@ -704,10 +707,10 @@ template <int D> hipError_t draft_dispatch(const DraftArgs &a, hipStream_t s) {
   }
 }
 template <int D> hipError_t draft_merge_dispatch(const DraftArgs &a, hipStream_t s) {
-  const dim3 grid(a.total * a.hq);
-  // few rows: more waves for each, since they may be split over the whole chip
-  if ((int64_t)a.total * a.hq <= 2048) hipLaunchKernelGGL((k_draft_merge<D, 4>), grid, dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((k_draft_merge<D, 1>), grid, dim3(64), 0, s, a);
+  const int64_t rows = (int64_t)a.total * a.hq;
+  constexpr int per_wg = 1024 / D;
+  if (rows <= 2048) hipLaunchKernelGGL((k_draft_merge<D, true>), dim3(rows), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((k_draft_merge<D, false>), dim3((rows + per_wg - 1) / per_wg), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
