@@ -1987,8 +1987,9 @@ namespace {
 // of an eight-wave workgroup idle, and a block takes it about as long with one
 // wave at work as with eight.  Those run tiles of 128, the large trees several
 // (12 trees of 5 to 61 nodes over 3K to 61K tokens of an 8-bit store: 303 us in
-// tiles of 256, 246 in tiles of 128, 291 with a launch for each size of tree; 186
-// now that an 8-bit store's tiles of up to 64 rows are streamed inside that launch).
+// tiles of 256, 246 in tiles of 128, 291 with a launch for each size of tree; 159
+// to 180 now that an 8-bit store's tiles of up to 64 rows are streamed inside that
+// launch and the runs are weighed as below).
 struct DraftShape {
   int32_t rows = 0, n_wg = 0, shared = 0;
 };
@@ -2013,37 +2014,53 @@ struct DraftTile {
   int64_t blocks;
 };
 // The tiles' blocks (for every KV head) dealt out to the workgroups in runs of
-// equal time: a block of a 128-row tile takes 10 with one wave at work, 13 with
-// four; in an 8-bit store 6 and 9 where it is streamed (up to 32 and 64 rows), 14
-// and 16 where not; others about the same whatever the rows; the start of a row,
-// kRowStart blocks.
-constexpr int64_t kRowStart = 1;
+// equal time: a block of a 128-row tile takes 20 with one wave at work, 23 with
+// four (with 26 the mixed batches below took 1.5% longer); in an 8-bit store 12 and
+// 18 where it is streamed (up to 32 and 64 rows), 30 and 32 where not; others about
+// the same whatever the rows.  The start of a row takes a block, three of a full
+// round of 128-row tiles (a piece more costs a workgroup 4 us at 64 channels, 8 at
+// 128, timed by their clocks).
+//
+// Of such a round's two workgroups on a CU the first one's waves are older and
+// issue first: with equal shares they ended at 130 us, the others at 164 (8-bit, 32
+// nodes over 8 x 22673 tokens; 64 channels, 16 nodes: 86 and 113).  So the first
+// get a fifth more and the others a fifth less: with the starts, nine mixed and
+// windowed batches 125 -> 117 us (geometric mean; the 12 trees above 167 -> 159).
+// 128 channels of bf16 wait for HBM and end together (12 trees 206 us so, 228 with
+// a tenth), and so do tiles of up to 64 rows (16 nodes over 8 x 22673 tokens 125
+// and 139).
+constexpr int64_t kEarly = 200; // of 1000
 // A workgroup takes three blocks at least, one (of a 256-row tile two) while there
 // is a CU for each: 12 nodes over 1000 tokens 20.3 us with three, 15.7 with one;
 // past a workgroup a CU, 30 over 4 x 1500 tokens 27 with three, 33 with one.
 constexpr int64_t kMinRun = 3;
-int32_t draft_split(const std::vector<DraftTile> &tiles, int hkv, int G, bool kv8, const DraftShape &shape,
+int32_t draft_split(const std::vector<DraftTile> &tiles, int hkv, int G, int D, bool kv8, const DraftShape &shape,
                     int cus, sq::DraftSplit *out) {
   auto weight = [&](const DraftTile &t) -> int64_t {
     const int waves = (t.as.n_nodes * G + 31) / 32;
-    static constexpr int w8[4] = {6, 9, 14, 16};
-    return shape.rows != 128 ? 10 : kv8 ? w8[waves - 1] : 10 + waves - 1;
+    static constexpr int w8[4] = {12, 18, 30, 32};
+    return shape.rows != 128 ? 20 : kv8 ? w8[waves - 1] : 20 + waves - 1;
   };
-  int64_t total = 0, blocks = 0;
-  for (const DraftTile &t : tiles) {
-    total += (t.blocks * weight(t) + kRowStart * 10) * hkv;
-    blocks += t.blocks * hkv;
-  }
+  int64_t blocks = 0;
+  for (const DraftTile &t : tiles) blocks += t.blocks * hkv;
   // a workgroup leaves two partial tiles at most, and all together one each and
   // one for every row
   const int64_t most = (int64_t)sq::kMaxItems * sq::kRows / shape.rows;
   const int64_t fit = std::max(most / 2, most - (int64_t)tiles.size() * hkv);
   const int64_t runs = std::max(blocks / kMinRun, std::min<int64_t>(cus, blocks / (shape.rows == 256 ? 2 : 1)));
   const int64_t n = std::max<int64_t>(1, std::min<int64_t>({shape.n_wg, fit, runs}));
+  const bool pairs = shape.rows == 128 && n == 2 * cus;
+  const int64_t start = pairs ? 60 : 20; // of a row
+  int64_t total = 0;
+  for (const DraftTile &t : tiles) total += (t.blocks * weight(t) + start) * hkv;
   int32_t extra = (int32_t)n, slots = 0; // pieces behind the workgroups' first ones
   int64_t w = 0, at = 0;                 // the workgroup at `at`, and its last piece
   int32_t last = -1;
-  auto end_of = [&](int64_t x) { return (x + 1) * total / n; };
+  const int64_t skew = pairs && (kv8 || D == 64) ? kEarly : 0;
+  auto end_of = [&](int64_t x) {
+    const int64_t early = std::min<int64_t>(x + 1, cus), late = x + 1 - early;
+    return (early * (1000 + skew) + late * (1000 - skew)) * total / (1000 * n);
+  };
   for (int64_t i = 0; i < n; ++i) {
     out->pieces[i] = sq::DraftPiece{};
     out->pieces[i].next = -1; // (without blocks, unless it gets some below)
@@ -2052,13 +2069,13 @@ int32_t draft_split(const std::vector<DraftTile> &tiles, int hkv, int G, bool kv
   for (size_t t = 0; t < tiles.size(); ++t) {
     const int64_t wt = weight(tiles[t]), nb = tiles[t].blocks;
     for (int g = 0; g < hkv; ++g) {
-      const int64_t stop = at + nb * wt + kRowStart * 10;
+      const int64_t stop = at + nb * wt + start;
       mine.clear();
       for (int64_t b = 0; b < nb;) {
         while (w + 1 < n && end_of(w) <= at) ++w, last = -1;
         const int64_t x = end_of(w);
         int64_t e = nb;
-        if (x < stop && w + 1 < n) e = std::min(nb, std::max(b, (x - (stop - nb * wt - kRowStart * 10) + wt / 2) / wt));
+        if (x < stop && w + 1 < n) e = std::min(nb, std::max(b, (x - (stop - nb * wt - start) + wt / 2) / wt));
         if (e > b) {
           const int32_t p = last < 0 ? (int32_t)w : extra++;
           if (last >= 0) out->pieces[last].next = p;
@@ -2285,7 +2302,7 @@ sq_status open_tokens(sq_store *s, const sq_seq *seqs, const int32_t *counts, in
     part(bl->nodes, total * sizeof(sq::DraftNode));
     for (int w = 0; w < (o.window > 0 ? 2 : 1); ++w) {
       sq::DraftSplit &sp = bl->split[w];
-      const int32_t n_pieces = draft_split(tiles[w], s->cfg.num_kv_heads, s->G, s->kv8, shape, s->cus, &sp);
+      const int32_t n_pieces = draft_split(tiles[w], s->cfg.num_kv_heads, s->G, s->D, s->kv8, shape, s->cus, &sp);
       part(&sp.n_used, 16);
       part(sp.merge, tiles[w].size() * s->cfg.num_kv_heads * sizeof(sq::DraftMerge));
       part(sp.pieces, n_pieces * sizeof(sq::DraftPiece));
