@@ -16,7 +16,13 @@
  *     shared, compacted cache: GQA split-K flash decoding plus a cross-split
  *     merge, and a multi-query MFMA tile for a prefix that several queries
  *     share (sq_decode_attn; the memory-bound step of §1 and §3.4, whose
- *     shared-prefix optimisation §3.4 points to).
+ *     shared-prefix optimisation §3.4 points to),
+ *   - the calls of a layered model around them: a chunk's slots taken before
+ *     its keys exist (sq_reserve), each layer's projections normed, rotated
+ *     and stored (sq_qkv_store, sq_qk_rope), attention of the chunk
+ *     (sq_extend_attn), and the verification of drafted tokens: a tree per
+ *     sequence attends in one pass and one path of it is kept (sq_draft_begin,
+ *     sq_draft_attn, sq_draft_accept; sq_truncate).
  *
  * Conventions for every call
  * --------------------------
@@ -548,8 +554,9 @@ typedef struct sq_qk_opts {
  * [n][num_kv_heads][D], packed, which may be q and k themselves where those
  * are packed.  opts NULL: a copy.  Needs no store; work is enqueued on
  * stream.  n = 0 does nothing.  SQ_ERR_INVALID: n outside [0, 2^24], head
- * counts outside [1, 65536], D other than 64 or 128, q, k, q_out or k_out null or not 16-byte aligned,
- * positions null or not 4-byte aligned, a bad stride or option. */
+ * counts outside [1, 65536], D other than 64 or 128, q, k, q_out or k_out
+ * null or not 16-byte aligned, positions null or not 4-byte aligned, a bad
+ * stride or option. */
 sq_status sq_qk_rope(const void *q, int64_t q_stride, const void *k, int64_t k_stride,
                      const int32_t *positions, int32_t n, int32_t num_q_heads,
                      int32_t num_kv_heads, int32_t head_dim, const sq_qk_opts *opts, void *q_out,
