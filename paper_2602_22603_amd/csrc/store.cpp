@@ -1989,18 +1989,26 @@ namespace {
 // (12 trees of 5 to 61 nodes over 3K to 61K tokens of an 8-bit store: 303 us in
 // tiles of 256, 246 in tiles of 128, 291 with a launch for each size of tree; 159
 // to 180 now that an 8-bit store's tiles of up to 64 rows are streamed inside that
-// launch and the runs are weighed as below).
+// launch and the runs are weighed as below).  For the same reason trees whose rows
+// end in a small tile run tiles of 128 in an 8-bit store, by the measured times of a
+// block: 60 for a full 256-row tile, 56 for a part, kBlock8 for 128 rows and less (8
+// x 22673 tokens, 40 nodes 231 us in tiles of 256, 198 in tiles of 128, 64 nodes
+// 257 and 274; a bf16 store 223 and 261, 273 and 282).
+constexpr int kBlock8[5] = {0, 12, 18, 30, 32}; // 8-bit store, 128-row tiles, by waves at work
 struct DraftShape {
   int32_t rows = 0, n_wg = 0, shared = 0;
 };
 DraftShape draft_shape(const sq_store *s, const int32_t *counts, int32_t batch) {
-  int32_t most = 0, least = INT32_MAX;
+  int32_t most = 0, least = INT32_MAX, by128 = 0, by256 = 0;
   for (int b = 0; b < batch; ++b) {
-    most = std::max(most, counts[b] * s->G);
-    least = std::min(least, counts[b] * s->G);
+    const int32_t r = counts[b] * s->G;
+    most = std::max(most, r);
+    least = std::min(least, r);
+    by128 += r / 128 * kBlock8[4] + kBlock8[(r % 128 + 31) / 32];
+    by256 += r / 256 * 60 + (r % 256 ? 56 : 0);
   }
   DraftShape d;
-  d.rows = most <= 64 ? 64 : least > 128 ? 256 : 128;
+  d.rows = most <= 64 ? 64 : least > 128 && !(s->kv8 && by128 < by256) ? 256 : 128;
   if (s->kv8 && most <= 64) d.rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
   d.shared = most > d.rows;
   const int per_cu = d.rows == 256 ? 1 : d.rows == 64 && s->D == 64 && !s->kv8 ? 3 : 2;
@@ -2038,8 +2046,7 @@ int32_t draft_split(const std::vector<DraftTile> &tiles, int hkv, int G, int D, 
                     int cus, sq::DraftSplit *out) {
   auto weight = [&](const DraftTile &t) -> int64_t {
     const int waves = (t.as.n_nodes * G + 31) / 32;
-    static constexpr int w8[4] = {12, 18, 30, 32};
-    return shape.rows != 128 ? 20 : kv8 ? w8[waves - 1] : 20 + waves - 1;
+    return shape.rows != 128 ? 20 : kv8 ? kBlock8[waves] : 20 + waves - 1;
   };
   int64_t blocks = 0;
   for (const DraftTile &t : tiles) blocks += t.blocks * hkv;

@@ -166,6 +166,18 @@ def test_trees_over_ragged_caches(sq, hq, hkv, d, kv8):
         b.check(sinks=True)
 
 
+@pytest.mark.parametrize("kv8", [False, True])
+@pytest.mark.parametrize("sizes", [[40, 33, 48, 36], [64, 60, 64, 56], [33, 64, 34, 35]])
+@pytest.mark.parametrize("hq,hkv,d", [(32, 8, 128), (16, 2, 64)])
+def test_trees_of_more_rows_than_a_tile(sq, hq, hkv, d, sizes, kv8):
+    """Every tree needs more than 128 rows, its last tile full, half full or
+    nearly empty."""
+    b = Batch(sq, hq, hkv, d, [0, 1111, 64, 5003], sizes, kv8, seed=sum(sizes), poison=True)
+    b.begin(window=700, first=70)
+    b.check(sinks=True)
+    b.check(window=700, first=70)
+
+
 @pytest.mark.parametrize("window,first", [(1, 0), (1, 1), (5, 0), (5, 4), (64, 1), (64, 64), (100, 131), (300, 4),
                                           (5000, 4), (16, 3000)])
 @pytest.mark.parametrize("hq,hkv,d,kv8", [(32, 8, 128, False), (64, 8, 64, True), (4, 4, 64, False)])
