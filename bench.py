@@ -62,8 +62,8 @@ def parse_args():
 GRAPH_TIMINGS = True
 
 
-DECODE_SOURCES = ("decode_kernels.hip", "decode_args.hpp", "sq_common.hpp", "fp8.hpp")
-EXTEND_SOURCES = ("extend_kernels.hip", "extend_args.hpp", "sq_common.hpp", "fp8.hpp")
+DECODE_SOURCES = ("decode_kernels.hip", "decode_args.hpp", "page_frags.hpp", "sq_common.hpp", "fp8.hpp")
+EXTEND_SOURCES = ("extend_kernels.hip", "extend_args.hpp", "attn_tile.hpp", "sq_common.hpp", "fp8.hpp")
 
 
 def kernel_sha(files=DECODE_SOURCES):
