@@ -23,7 +23,8 @@ constexpr int P = kPage;
 // ---------------------------------------------------------------------------
 // One launch per opening: the plan's parts come from pinned host memory by a
 // kernel (a copy-engine transfer costs 10 us of hand-over), page-table entries
-// and positions go out in the same launch.  Bound by latency: a few KB.
+// and positions go out in the same launch.  Bound by latency: 4 us for a chunk, 7 for
+// eight trees of 64 nodes (50 KB).
 __global__ __launch_bounds__(256) void k_open(OpenArgs a, int32_t copy_blocks) {
   if ((int)blockIdx.x < copy_blocks) {
     int i = blockIdx.x * 256 + threadIdx.x;
