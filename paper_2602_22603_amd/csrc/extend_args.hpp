@@ -52,7 +52,7 @@ struct ExtendArgs {
   int32_t kv8;        // 1: the pools hold E4M3 codes (K scale in scale_log2)
   float out_scale;    // the layer's V scale in an 8-bit store (1 otherwise)
   int32_t rows;       // query rows per workgroup, 32 per wave: 256, 128 or 64
-  int32_t first;      // a window's queries also see the keys below this
+  int32_t first;      // a window's queries also see the keys below this (at most L)
 };
 
 static_assert(sizeof(ExtendArgs) < 4096, "extend kernel arguments too large");

@@ -2917,7 +2917,9 @@ sq_status sq_extend_attn_ex(sq_store *s, int32_t layer, sq_seq seq, int32_t n_ne
   a.scale_log2 = (float)((double)scale * 1.4426950408889634 * (double)s->k_scale(layer));
   a.sinks = o.sinks;
   a.window = o.window;
-  a.first = o.window > 0 ? o.first : 0;
+  // first tokens past the sequence's end are its every key (the kernel rounds
+  // first up to whole blocks in 32 bits)
+  a.first = o.window > 0 ? (int32_t)std::min<int64_t>(o.first, sqn->length) : 0;
   a.sink_scale = 1.4426950408889634f;
   a.kv8 = s->kv8 ? 1 : 0;
   a.out_scale = s->v_scale(layer);
