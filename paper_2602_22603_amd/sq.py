@@ -220,9 +220,22 @@ def trace_open(path):
     _check(lib().sq_trace_open(None if path is None else str(path).encode()))
 
 
+def _i32(x, what):
+    """int(x), refused where a 32-bit argument would wrap to another value."""
+    x = int(x)
+    if -0x80000000 <= x <= 0x7FFFFFFF:
+        return x
+    raise SqError(ERR_INVALID, f"{what} {x} is no 32-bit integer")
+
+
 def _i32_array(values):
-    arr = (C.c_int32 * max(1, len(values)))(*[int(v) for v in values])
-    return arr
+    """The values as an array for a call (through array(), which refuses what 32
+    bits do not hold, where ctypes would wrap it)."""
+    try:
+        a = array("i", map(int, values)) or array("i", (0,))
+    except OverflowError:
+        raise SqError(ERR_INVALID, f"not 32-bit integers: {values}") from None
+    return (C.c_int32 * len(a)).from_buffer(a)
 
 
 def _i32_joined(lists):
@@ -454,8 +467,8 @@ class Store:
         if not window and sinks is None and not first:
             return None
         o = AttnOpts()
-        o.window = int(window)
-        o.first = int(first)
+        o.window = _i32(window, "window")
+        o.first = _i32(first, "first")
         if sinks is not None:
             o.sinks = (_ptr(sinks) if self.metadata_only else
                        self._tensor(sinks, (self.num_q_heads,), torch.float32, "sinks"))
@@ -579,7 +592,7 @@ class Store:
                                             C.byref(o), st))
         elif window:
             _check(lib().sq_step_begin_ex(self._handle, _i32_array(seqs), len(seqs), mode,
-                                          int(window), st))
+                                          _i32(window, "window"), st))
         else:
             _check(lib().sq_step_begin(self._handle, _i32_array(seqs), len(seqs), mode, st))
         self._step_batch = len(seqs)
@@ -672,14 +685,17 @@ class Store:
             q_out = torch.empty((n, hq, dim), dtype=torch.bfloat16, device=dev)
         qo = _packed(q_out, (n, hq, dim), torch.bfloat16, dev, "q_out")
         o = _qk_opts(dim, dev, inv_freq, q_weight, k_weight, eps, interleaved, mscale)
-        _check(lib().sq_qkv_store(self._handle, layer, qp, qs, kp, ks, vp, vs,
+        _check(lib().sq_qkv_store(self._handle, _i32(layer, "layer"), qp, qs, kp, ks, vp, vs,
                                   None if o is None else C.byref(o), qo, _stream(stream)))
         return q_out
 
     def truncate(self, seq, length, stream=None):
         """Drop the tokens of seq from index `length` on."""
+        length = int(length)
+        if not -(1 << 63) <= length < 1 << 63:
+            raise SqError(ERR_INVALID, f"length {length} is no 64-bit integer")
         st = C.c_void_p(0) if self.metadata_only else _stream(stream)
-        _check(lib().sq_truncate(self._handle, seq, int(length), st))
+        _check(lib().sq_truncate(self._handle, _i32(seq, "sequence"), length, st))
 
     # -- drafted tokens ------------------------------------------------------------
     def draft_begin(self, seqs, parents, window=0, first=0, stream=None):
@@ -717,7 +733,7 @@ class Store:
             scale = 1.0 / float(self.head_dim) ** 0.5
         qp, op = self._qo_ptrs(q, out, n)
         o = self._opts(window, sinks, first if window else 0)
-        _check(lib().sq_draft_attn(self._handle, layer, qp, op, float(scale),
+        _check(lib().sq_draft_attn(self._handle, _i32(layer, "layer"), qp, op, float(scale),
                                    None if o is None else C.byref(o), _stream(stream)))
         return out
 
@@ -744,7 +760,7 @@ class Store:
     def extend_plan_info(self, seq, n, window=0):
         """How extend() would cut the last n tokens of seq into workgroups."""
         ei = ExtendInfo()
-        _check(lib().sq_extend_plan_info(self._handle, seq, n, window, C.byref(ei)))
+        _check(lib().sq_extend_plan_info(self._handle, seq, n, _i32(window, "window"), C.byref(ei)))
         return {n: getattr(ei, n) for n, _ in ExtendInfo._fields_}
 
     # -- introspection -------------------------------------------------------------
