@@ -703,6 +703,7 @@ class Store:
         tree (an earlier node, or -1).  window, first: of the layers that will
         be windowed."""
         seqs = list(seqs)
+        parents = [list(p) for p in parents]
         counts = [len(p) for p in parents]
         if len(seqs) != len(counts):
             raise SqError(ERR_INVALID, "one tree for each sequence")
