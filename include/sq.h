@@ -563,13 +563,16 @@ sq_status sq_qk_rope(const void *q, int64_t q_stride, const void *k, int64_t k_s
                      void *k_out, void *stream);
 
 /* Append counts[b] tokens' slots to each of `batch` distinct sequences: pages
- * in batch order, positions as sq_append.  Until the next call that changes a
- * sequence of the store the tokens are open: sq_qkv_store takes their K and V
- * layer by layer.  A slot whose layer has not been stored holds stale values.
+ * in batch order, positions as sq_append.  Until the next call that changes the
+ * slots of a sequence of the store (append, fork, release, eviction, truncation,
+ * a new step, reservation or draft; a refused call changes none, and neither
+ * does an eviction that finds nothing to evict) the tokens are open: sq_qkv_store
+ * takes their K and V layer by layer.  A slot whose layer has not been stored holds stale values.
  * sq_reserve errors change nothing.  SQ_ERR_INVALID: batch outside [1,
  * SQ_MAX_BATCH], a repeated sequence, a count < 1, more than SQ_MAX_RESERVE
  * tokens, a sequence past its page-list capacity, positions past int32, an
- * open draft, a stream in capture; SQ_ERR_NO_PAGES.  A metadata-only store changes its metadata. */
+ * open draft, a stream in capture; SQ_ERR_NO_PAGES.  A metadata-only store
+ * changes its metadata. */
 #define SQ_MAX_RESERVE 262144
 sq_status sq_reserve(sq_store *store, const sq_seq *seqs, const int32_t *counts, int32_t batch,
                      void *stream);

@@ -1548,7 +1548,7 @@ namespace {
 // Deferred eviction: the spans' slots are masked, nothing moves.
 sq_status evict_deferred(sq_store *s, sq_seq h, const std::vector<int32_t> &ids,
                          const std::vector<std::pair<int64_t, int64_t>> &sp, void *stream,
-                         sq_evict_stats *stats) {
+                         sq_evict_stats *stats, bool *changed) {
   if (s->P > 16) return fail(SQ_ERR_INVALID, "deferred eviction needs page_size <= 16");
   Seq *q = s->get(h);
   std::vector<uint16_t> km = q->kmask;
@@ -1574,6 +1574,7 @@ sq_status evict_deferred(sq_store *s, sq_seq h, const std::vector<int32_t> &ids,
       break;
     }
   es.tokens_masked = newly;
+  *changed = newly > 0;
   q->kmask = std::move(km);
   q->n_masked += newly;
   if (q->n_masked == 0) q->kmask.clear();
@@ -1644,13 +1645,10 @@ sq_status evict_inplace_launches(sq_store *s, sq_seq h, int64_t fp, int64_t n_ne
 
 } // namespace
 
-sq_status sq_evict_spans_ex(sq_store *s, sq_seq h, const int32_t *cursor_ids, int32_t n,
-                            uint32_t flags, void *stream, sq_evict_stats *stats) {
-  SQ_TRACE_CALL("sq_evict_spans", "store=%p seq=%d n_cursors=%d flags=%u", (void *)s, h, n, flags);
-  if (!s) return fail(SQ_ERR_INVALID, "null store");
+// sq_evict_spans_ex on a live sequence; *changed: a slot was masked or moved.
+static sq_status evict_spans(sq_store *s, sq_seq h, const int32_t *cursor_ids, int32_t n, uint32_t flags,
+                             void *stream, sq_evict_stats *stats, bool *changed) {
   Seq *q = s->get(h);
-  if (!q) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", h);
-  ++s->gen; // ends a begun decode step even when the call fails
   if (sq_status r = no_draft(*q, h)) return r;
   if (n < 0 || n > SQ_MAX_EVICT_SPANS)
     return fail(SQ_ERR_INVALID, "cursor count %d outside [0, %d]", n, SQ_MAX_EVICT_SPANS);
@@ -1667,7 +1665,7 @@ sq_status sq_evict_spans_ex(sq_store *s, sq_seq h, const int32_t *cursor_ids, in
     if (se.second > se.first) sp.push_back(se);
   }
   std::sort(sp.begin(), sp.end());
-  if (flags & SQ_EVICT_DEFER) return evict_deferred(s, h, ids, sp, stream, stats);
+  if (flags & SQ_EVICT_DEFER) return evict_deferred(s, h, ids, sp, stream, stats, changed);
   if (q->n_masked > 0) {
     // masked slots leave with the spans: the union, as maximal runs
     std::vector<std::pair<int64_t, int64_t>> all = masked_runs(*q, s->P);
@@ -1788,6 +1786,7 @@ sq_status sq_evict_spans_ex(sq_store *s, sq_seq h, const int32_t *cursor_ids, in
   // ---- commit: allocate and release in schedule order, enqueue the device
   // work (stream order keeps every gather ahead of the reuse of what it read),
   // then the host bookkeeping ----
+  *changed = true;
   std::vector<int32_t> new_ids(n_new);
   int64_t freed = 0;
   for (int64_t k = 0; k < n_new; ++k)
@@ -1973,6 +1972,19 @@ sq_status sq_evict_spans_ex(sq_store *s, sq_seq h, const int32_t *cursor_ids, in
   s->st.evict_bytes_moved += es.bytes_moved;
   if (stats) *stats = es;
   return SQ_OK;
+}
+
+sq_status sq_evict_spans_ex(sq_store *s, sq_seq h, const int32_t *cursor_ids, int32_t n,
+                            uint32_t flags, void *stream, sq_evict_stats *stats) {
+  SQ_TRACE_CALL("sq_evict_spans", "store=%p seq=%d n_cursors=%d flags=%u", (void *)s, h, n, flags);
+  if (!s) return fail(SQ_ERR_INVALID, "null store");
+  if (!s->get(h)) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", h);
+  const bool chunk = s->open.kind == sq_store::Open::kChunk && s->open.gen == s->gen;
+  ++s->gen; // ends a begun decode step even when the call fails
+  bool changed = false;
+  const sq_status r = evict_spans(s, h, cursor_ids, n, flags, stream, stats, &changed);
+  if (chunk && !changed) s->open.gen = s->gen; // reserved tokens stay open unless slots changed
+  return r;
 }
 
 // ---- tokens whose K and V come layer by layer --------------------------------
