@@ -66,7 +66,7 @@
 extern "C" {
 #endif
 
-#define SQ_ABI_VERSION 9
+#define SQ_ABI_VERSION 10
 
 typedef struct sq_store sq_store; /* opaque, library-owned host metadata */
 typedef int32_t sq_seq;           /* sequence handle: main thread or aux branch */
@@ -659,11 +659,16 @@ sq_status sq_decode_plan_info(sq_store *store, const sq_seq *seqs, int32_t batch
                               int32_t mode, sq_plan_info *out);
 
 /* Host-only description of how sq_extend_attn_ex would cut the last n_new
- * tokens of seq with this window (0: none) into workgroups.  A metadata-only
- * store answers for a GPU of 256 compute units.  SQ_ERR_INVALID: n_new
- * outside [1, length], window < 0, a head shape without a kernel. */
+ * tokens of seq with this window (0: none) and no first tokens into
+ * workgroups.  A metadata-only store answers for a GPU of 256 compute units.
+ * SQ_ERR_INVALID: n_new outside [1, length], window < 0, a head shape without
+ * a kernel. */
 sq_status sq_extend_plan_info(sq_store *store, sq_seq seq, int32_t n_new, int32_t window,
                               sq_extend_info *out);
+
+/* The same with the options of that call (window and first count; NULL: none). */
+sq_status sq_extend_plan_info_opts(sq_store *store, sq_seq seq, int32_t n_new,
+                                   const sq_attn_opts *opts, sq_extend_info *out);
 
 /* ---- introspection -------------------------------------------------------*/
 sq_status sq_seq_info(sq_store *store, sq_seq seq, sq_seq_desc *out);

@@ -2887,6 +2887,12 @@ sq_status sq_step_attn_ex(sq_store *s, int32_t layer, const void *k_new, const v
   return SQ_OK;
 }
 
+// The first tokens of a windowed extend call: past the sequence's end they are its
+// every key (the kernel rounds them up to whole blocks in 32 bits).
+static int32_t extend_first(const sq_attn_opts &o, int64_t L) {
+  return o.window > 0 ? (int32_t)std::min<int64_t>(o.first, L) : 0;
+}
+
 sq_status sq_extend_attn(sq_store *s, int32_t layer, sq_seq seq, int32_t n_new, const void *q,
                          float *out, float scale, void *stream) {
   return sq_extend_attn_ex(s, layer, seq, n_new, q, out, scale, nullptr, stream);
@@ -2929,9 +2935,7 @@ sq_status sq_extend_attn_ex(sq_store *s, int32_t layer, sq_seq seq, int32_t n_ne
   a.scale_log2 = (float)((double)scale * 1.4426950408889634 * (double)s->k_scale(layer));
   a.sinks = o.sinks;
   a.window = o.window;
-  // first tokens past the sequence's end are its every key (the kernel rounds
-  // first up to whole blocks in 32 bits)
-  a.first = o.window > 0 ? (int32_t)std::min<int64_t>(o.first, sqn->length) : 0;
+  a.first = extend_first(o, sqn->length);
   a.sink_scale = 1.4426950408889634f;
   a.kv8 = s->kv8 ? 1 : 0;
   a.out_scale = s->v_scale(layer);
@@ -2962,15 +2966,24 @@ sq_status sq_extend_attn_ex(sq_store *s, int32_t layer, sq_seq seq, int32_t n_ne
 }
 
 sq_status sq_extend_plan_info(sq_store *s, sq_seq h, int32_t n_new, int32_t window, sq_extend_info *out) {
+  sq_attn_opts o{};
+  o.window = window;
+  return sq_extend_plan_info_opts(s, h, n_new, &o, out);
+}
+
+sq_status sq_extend_plan_info_opts(sq_store *s, sq_seq h, int32_t n_new, const sq_attn_opts *opts,
+                                   sq_extend_info *out) {
   if (!s || !out) return fail(SQ_ERR_INVALID, "null argument");
   const Seq *q = s->get(h);
   if (!q) return fail(SQ_ERR_UNKNOWN_SEQ, "unknown sequence %d", h);
   if (n_new < 1 || n_new > q->length)
     return fail(SQ_ERR_INVALID, "n_new %d outside [1, %lld]", n_new, (long long)q->length);
-  if (window < 0) return fail(SQ_ERR_INVALID, "window %d < 0", window);
+  sq_attn_opts o{};
+  sq_status r = take_opts(opts, &o);
+  if (r != SQ_OK) return r;
   if ((s->D != 64 && s->D != 128) || (s->G != 1 && s->G != 2 && s->G != 4 && s->G != 8))
     return fail(SQ_ERR_INVALID, "no extend kernel for head_dim %d and %d query heads per KV head", s->D, s->G);
-  const ExtendPlan ep = plan_extend(s, n_new, q->length, window);
+  const ExtendPlan ep = plan_extend(s, n_new, q->length, o.window, extend_first(o, q->length));
   out->rows = ep.rows;
   out->n_qblocks = ep.n_qblocks;
   out->n_split = ep.n_split;

@@ -174,6 +174,8 @@ _SIGS = {
                                       C.POINTER(PlanInfo)]),
     "sq_extend_plan_info": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int32,
                                       C.POINTER(ExtendInfo)]),
+    "sq_extend_plan_info_opts": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.POINTER(AttnOpts),
+                                           C.POINTER(ExtendInfo)]),
     "sq_seq_info": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(SeqDesc)]),
     "sq_page_table": (C.c_int, [C.c_void_p, C.c_int32, C.POINTER(C.c_int32), C.c_int32,
                                 C.POINTER(C.c_int32)]),
@@ -758,10 +760,12 @@ class Store:
                                          C.byref(pi)))
         return {n: getattr(pi, n) for n, _ in PlanInfo._fields_}
 
-    def extend_plan_info(self, seq, n, window=0):
+    def extend_plan_info(self, seq, n, window=0, first=0):
         """How extend() would cut the last n tokens of seq into workgroups."""
         ei = ExtendInfo()
-        _check(lib().sq_extend_plan_info(self._handle, seq, n, _i32(window, "window"), C.byref(ei)))
+        o = self._opts(window, None, first)
+        _check(lib().sq_extend_plan_info_opts(self._handle, seq, n, None if o is None else C.byref(o),
+                                              C.byref(ei)))
         return {n: getattr(ei, n) for n, _ in ExtendInfo._fields_}
 
     # -- introspection -------------------------------------------------------------
