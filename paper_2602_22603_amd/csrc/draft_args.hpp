@@ -49,8 +49,12 @@ struct DraftMerge {
 
 constexpr int kDraftRows = 4096; // (tile, KV head) rows
 constexpr int kDraftWgs = 1024;  // workgroups of a launch
+// A captured launch has its tile and its number of nodes from the draft it was
+// captured with; where the plan's are others it does nothing.
 struct DraftSplit {
-  int32_t n_used, pad[3];        // workgroups that have work
+  int32_t n_used;                // workgroups that have work (0: no such plan)
+  int32_t rows, total;           // query rows of a tile, nodes in all
+  int32_t pad;
   DraftMerge merge[kDraftRows];
   DraftPiece pieces[kDraftRows + kDraftWgs];
 };

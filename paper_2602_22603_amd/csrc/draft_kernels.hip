@@ -41,6 +41,14 @@ struct PieceRef {
   }
 };
 
+// Whether a launch was laid out for this plan: the rows of its tiles and the nodes
+// of q and out.  (A captured one may be replayed while another draft is open: its
+// partial rows would lie past the workspace, its nodes past q and out.)
+__device__ inline bool fits(const DraftArgs &a, const DraftSplit &sp) {
+  const ext_sptr_t x = (ext_sptr_t)&sp.n_used;
+  return (int)blockIdx.x < x[0] && x[1] == a.rows && x[2] == a.total;
+}
+
 // The pages of one sequence.
 struct SeqPages {
   const int32_t *pt;
@@ -95,7 +103,7 @@ __device__ inline void stream_piece(const DraftArgs &a, const PieceRef &pc, cons
   const int rg = wave % RG, kpart = wave / RG;
   const int plan = a.windowed;
   const int g = pc.g, base = pc.base, n_draft = pc.n, n_pages = pc.n_pages, node0 = pc.node0;
-  const int n_nodes = min(pc.n_nodes, a.total - node0); // (in a replay for a larger draft none past q and out)
+  const int n_nodes = pc.n_nodes;
   const int masked = pc.masked, nf = pc.nf, skip = pc.skip, lo_max = pc.lo_max, b_lo = pc.b_lo, b_hi = pc.b_hi;
   const int slot = pc.slot, pt_row = pc.row;
   const int L = base + n_draft;
@@ -369,8 +377,8 @@ k_draft_stream(DraftArgs a) {
   __shared__ uint64_t s_anc[kMaxDraft];
   __shared__ int32_t s_lo[kMaxDraft];
   const DraftSplit &sp = a.blob->split[a.windowed];
+  if (!fits(a, sp)) return;
   int next = blockIdx.x;
-  if (next >= *(ext_sptr_t)&sp.n_used) return;
   while (next >= 0) {
     const PieceRef pc(sp.pieces[next]);
     next = pc.next;
@@ -407,12 +415,12 @@ k_draft(DraftArgs a) {
   const int n = lane & 15, kg = lane >> 4;
   const int plan = a.windowed;
   const DraftSplit &sp = a.blob->split[plan];
+  if (!fits(a, sp)) return;
   int next = blockIdx.x;
-  if (next >= *(ext_sptr_t)&sp.n_used) return;
   while (next >= 0) {
     const PieceRef pc(sp.pieces[next]);
     const int g = pc.g, base = pc.base, n_draft = pc.n, n_pages = pc.n_pages, node0 = pc.node0;
-    const int n_nodes = min(pc.n_nodes, a.total - node0); // (in a replay for a larger draft none past q and out)
+    const int n_nodes = pc.n_nodes;
     const int masked = pc.masked, nf = pc.nf, skip = pc.skip, lo_max = pc.lo_max, b_lo = pc.b_lo, b_hi = pc.b_hi;
     const int slot = pc.slot, pt_row = pc.row;
     next = pc.next;
@@ -624,8 +632,11 @@ __global__ __launch_bounds__(256) void k_draft_merge(DraftArgs a) {
   const int i = live ? r / a.hq : 0, h = live ? r % a.hq : 0;
   const int tile = a.blob->nodes[i].tile, in_tile = a.blob->nodes[i].in_tile;
   const int g = h >> a.lg;
-  const DraftMerge mr = a.blob->split[a.windowed].merge[tile * a.hkv + g];
-  if (!live || mr.n == 0) return; // (SHARED: the whole workgroup)
+  const DraftSplit &sp = a.blob->split[a.windowed];
+  const ext_sptr_t plan = (ext_sptr_t)&sp.n_used;
+  const bool fit = plan[1] == a.rows && plan[2] == a.total;
+  const DraftMerge mr = sp.merge[tile * a.hkv + g]; // (of another draft's plan at worst)
+  if (!live || !fit || mr.n == 0) return; // (SHARED: the whole workgroup)
   const int col = (in_tile << a.lg) + (h & ((1 << a.lg) - 1));
   float big = kNegInf, den = 0.f;
   float4 num = make_float4(0.f, 0.f, 0.f, 0.f);

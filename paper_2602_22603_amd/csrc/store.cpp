@@ -2119,6 +2119,7 @@ int32_t draft_split(const std::vector<DraftTile> &tiles, int hkv, int G, int D, 
     }
   }
   out->n_used = (int32_t)n;
+  out->rows = shape.rows;
   return extra;
 }
 
@@ -2319,8 +2320,14 @@ sq_status open_tokens(sq_store *s, const sq_seq *seqs, const int32_t *counts, in
   part(bl->ids, op.n_units * sizeof(int32_t));
   if (draft) {
     part(bl->nodes, total * sizeof(sq::DraftNode));
-    for (int w = 0; w < (o.window > 0 ? 2 : 1); ++w) {
+    for (int w = 0; w < 2; ++w) {
       sq::DraftSplit &sp = bl->split[w];
+      if (w == 1 && o.window == 0) { // no windowed plan: none left from the draft before
+        sp.n_used = sp.rows = sp.total = 0;
+        part(&sp.n_used, 16);
+        break;
+      }
+      sp.total = (int32_t)total;
       const int32_t n_pieces = draft_split(tiles[w], s->cfg.num_kv_heads, s->G, s->D, s->kv8, shape, s->cus, &sp);
       part(&sp.n_used, 16);
       part(sp.merge, tiles[w].size() * s->cfg.num_kv_heads * sizeof(sq::DraftMerge));
