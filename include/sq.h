@@ -35,7 +35,7 @@
  *  - Device buffers (pools, workspace, q, out, new K/V) are allocated and
  *    owned by the caller and must outlive the store or the call.  The library
  *    owns host metadata only; it never allocates device memory.  In device
- *    mode it allocates one pinned host staging buffer at sq_store_create.
+ *    mode it allocates pinned host staging buffers at sq_store_create.
  *  - Host metadata changes when a call returns; device work is enqueued on
  *    the given HIP stream (a hipStream_t passed as void*; NULL = the null
  *    stream).  All device work of one store must go to ONE stream, in call
@@ -471,7 +471,11 @@ sq_status sq_extend_attn(sq_store *store, int32_t layer, sq_seq seq, int32_t n_n
  *   first   F > 0: a windowed query also attends to the keys at indices 0 ..
  *           F - 1 (the sequence's first tokens stay visible however far the
  *           window has moved on; a key both name counts once).  Without a
- *           window every key is visible and F changes nothing.
+ *           window every key is visible and F changes nothing.  In a decode
+ *           call or step the first tokens of a sequence whose window has left
+ *           them behind are a range of pages of their own, and so many
+ *           (range, KV head) pairs have room: a call with 8192 or more (64
+ *           sequences with 64 KV heads, say) is SQ_ERR_INVALID.
  *   reserved, reserved2  must be 0.
  * The window is over logical indices of the (compacted) cache, as the
  * causal mask is.  SQ_ERR_INVALID: window < 0, first < 0, a reserved field
@@ -596,9 +600,8 @@ sq_status sq_qkv_store(sq_store *store, int32_t layer, const void *q, int64_t q_
  * position of the first dropped one.  A last page that ends up part full
  * while another branch holds it too is first copied to a new page.
  * SQ_ERR_INVALID: length outside [0, length of seq], an open draft on seq, a
- * stream in capture;
- * SQ_ERR_SPAN: a registered span ends past length; SQ_ERR_NO_PAGES: no page
- * for that copy. */
+ * stream in capture; SQ_ERR_SPAN: a registered span ends past length;
+ * SQ_ERR_NO_PAGES: no page for that copy. */
 sq_status sq_truncate(sq_store *store, sq_seq seq, int64_t length, void *stream);
 
 /* ---- drafted tokens ------------------------------------------------------
@@ -608,8 +611,8 @@ sq_status sq_truncate(sq_store *store, sq_seq seq, int64_t length, void *stream)
  * the nodes' K and V there and sq_draft_attn attends; sq_draft_accept keeps a
  * path of each tree and drops the rest.
  *
- * While a draft is open its sequences take no other call than introspection
- * (SQ_ERR_INVALID; accept empty paths to abandon it).  Other sequences do, but
+ * While a draft is open its sequences take no other call than introspection,
+ * which counts its nodes (SQ_ERR_INVALID; accept empty paths to abandon it).  Other sequences do, but
  * sq_reserve waits for its end.  Cached K and V must be finite, as for every
  * attention call: a masked value counts with weight 0. */
 #define SQ_MAX_DRAFT 64 /* nodes of one sequence */
@@ -624,8 +627,7 @@ sq_status sq_truncate(sq_store *store, sq_seq seq, int64_t length, void *stream)
  * count outside [1, SQ_MAX_DRAFT], a bad parent, an open draft, a sequence
  * past its page-list capacity, a window over masked slots, more than 4096
  * (sequence, KV head) rows of work, bad options, a stream in capture;
- * SQ_ERR_NO_PAGES.  Errors
- * change nothing. */
+ * SQ_ERR_NO_PAGES.  Errors change nothing. */
 sq_status sq_draft_begin(sq_store *store, const sq_seq *seqs, const int32_t *counts, int32_t batch,
                          const int32_t *parents, const sq_attn_opts *opts, void *stream);
 
@@ -639,8 +641,10 @@ sq_status sq_draft_begin(sq_store *store, const sq_seq *seqs, const int32_t *cou
  * opts->first.  opts->window is 0 or that of the begin, with its first; sinks
  * as in sq_attn_opts.  The launches depend on the arguments and the begin's
  * counts only: a capture replays for any later begin of the same counts,
- * window and first tokens.  SQ_ERR_INVALID: no open draft, bad layer, pointer
- * or options, scale not finite and positive, metadata-only store. */
+ * window and first tokens (with other counts open it may do nothing).  Weights
+ * are held as two bf16 halves, 16 bits.  SQ_ERR_INVALID: no open draft, bad
+ * layer, pointer or options, scale not finite and positive, metadata-only
+ * store. */
 sq_status sq_draft_attn(sq_store *store, int32_t layer, const void *q, float *out, float scale,
                         const sq_attn_opts *opts, void *stream);
 
