@@ -21,9 +21,15 @@
 // test.
 //
 // Measured, one layer of 32 + 8 heads of 128 channels: 16 nodes over 8 x 128K tokens
-// 620 us, 6.9 TB/s of K and V (HBM); 64 over 60547 tokens 98 us, 640 TFLOP/s useful
-// (matrix and vector work one after the other; 16-bit weights take half as many
-// products again); 5 over 2048 tokens 8.4 us and the merge 3.1 (a chain of reads).
+// 631 us, 6.8 TB/s of K and V (HBM); 64 over 60547 tokens 98-100 us, 640 TFLOP/s
+// useful (matrix and vector work one after the other; 16-bit weights take half as
+// many products again); 5 over 2048 tokens 8.6 us and the merge 3.5 (a chain of
+// reads).
+//
+// A weight is held as two bf16 halves, 16 bits, since the products take bf16: an
+// output is within 3e-6 of float64 in the 2-norm, two to four times as far as with
+// fp32 weights, where one half would be 1e-3 off and a third part would cost
+// another product of every weight and value.
 #include "attn_tile.hpp"
 #include "draft_args.hpp"
 #include "page_frags.hpp"
@@ -425,7 +431,7 @@ k_draft(DraftArgs a) {
     const int slot = pc.slot, pt_row = pc.row;
     next = pc.next;
     if (b_lo >= b_hi) continue; // (a workgroup without work)
-    if constexpr (kSmall) { // (a batch of mixed trees 237 us without, 186 with)
+    if constexpr (kSmall) { // (12 mixed trees 298 us without, 172 with)
       static_assert(Lt::K_ELEMS * 2 >= 32 * D * 4 && Lt::V_ELEMS * 2 >= 32 * D * 4, "a wave's accumulator in each");
       const StreamLds<32> lds{s_m, s_l, s_anc, s_lo};
       const SwizzledRows<D> states{reinterpret_cast<float *>(sk0), reinterpret_cast<float *>(sk1),
@@ -617,8 +623,8 @@ k_draft(DraftArgs a) {
 // 2^(m_s - M) l_s.  D / 4 lanes take a (node, head)'s slots, four channels each, a
 // workgroup 1024 / D of them; or, SHARED, all of a workgroup's lane groups take
 // shares of one row's slots, for few rows whose keys were split over the chip.
-// Bound by the partial rows it reads (64 nodes over 60547 tokens: 34 MB, 7.2 us)
-// and, below some MB, by a chain of four loads (3 us).  With a wave to a row, 13760
+// Bound by the partial rows it reads (64 nodes over 60547 tokens: 34 MB, 7.5 us)
+// and, below some MB, by a chain of four loads (3.5 us).  With a wave to a row, 13760
 // rows of 64 channels took 6.9 us, 5.8 so.
 template <int D, bool SHARED>
 __global__ __launch_bounds__(256) void k_draft_merge(DraftArgs a) {

@@ -35,13 +35,13 @@ inline bool tree_depths(const int32_t *parents, int32_t n, int32_t *depth) {
 // of an eight-wave workgroup idle, and a block takes it about as long with one
 // wave at work as with eight.  Those run tiles of 128, the large trees several
 // (12 trees of 5 to 61 nodes over 3K to 61K tokens of an 8-bit store: 303 us in
-// tiles of 256, 246 in tiles of 128, 291 with a launch for each size of tree; 159
-// to 180 now that an 8-bit store's tiles of up to 64 rows are streamed inside that
-// launch and the runs are weighed as below).  For the same reason trees whose rows
+// tiles of 256, 246 in tiles of 128, 291 with a launch for each size of tree; 172
+// now that an 8-bit store's tiles of up to 64 rows are streamed inside that launch
+// and the runs are weighed as below).  For the same reason trees whose rows
 // end in a small tile run tiles of 128 in an 8-bit store, by the measured times of a
 // block: 60 for a full 256-row tile, 56 for a part, kBlock8 for 128 rows and less (8
-// x 22673 tokens, 40 nodes 231 us in tiles of 256, 198 in tiles of 128, 64 nodes
-// 257 and 274; a bf16 store 223 and 261, 273 and 282).
+// x 22673 tokens, 40 nodes 230 us in tiles of 256, 203 in tiles of 128, 64 nodes
+// 257 and 275; a bf16 store 223 and 260, 271 and 280).
 constexpr int kBlock8[5] = {0, 12, 18, 30, 32}; // 8-bit store, 128-row tiles, by waves at work
 struct DraftShape {
   int32_t rows = 0, n_wg = 0, shared = 0;
@@ -141,11 +141,13 @@ inline int64_t draft_entry(const DraftEntry &e, int32_t window, int32_t first, c
 // Of such a round's two workgroups on a CU the first one's waves are older and
 // issue first: with equal shares they ended at 130 us, the others at 164 (8-bit, 32
 // nodes over 8 x 22673 tokens; 64 channels, 16 nodes: 86 and 113).  So the first
-// get a fifth more and the others a fifth less: with the starts, nine mixed and
-// windowed batches 125 -> 117 us (geometric mean; the 12 trees above 167 -> 159).
-// 128 channels of bf16 wait for HBM and end together (12 trees 206 us so, 228 with
-// a tenth), and so do tiles of up to 64 rows (16 nodes over 8 x 22673 tokens 125
-// and 139).
+// get a fifth more and the others a fifth less: the 12 trees above 180 -> 172 us, 16
+// windowed trees of 64 channels 54 -> 50.  128 channels of bf16 wait for HBM and end
+// together (12 such trees 232 us so, 236 with a tenth), and so do tiles of up to 64
+// rows (16 nodes over 8 x 22673 tokens 125 and 142).  Only for a full round: of
+// fewer workgroups the index does not say which share a CU.  (That it says so of a
+// full one is how the dispatcher hands workgroups out here; nothing but time
+// depends on it.)
 constexpr int64_t kEarly = 200; // of 1000
 // A workgroup takes three blocks at least, one (of a 256-row tile two) while there
 // is a CU for each: 12 nodes over 1000 tokens 20.3 us with three, 15.7 with one;
