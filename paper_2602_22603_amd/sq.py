@@ -12,6 +12,7 @@ import ctypes as C
 import os
 from array import array
 from itertools import chain
+from operator import index
 
 import numpy as np
 
@@ -687,7 +688,7 @@ class Store:
             q_out = torch.empty((n, hq, dim), dtype=torch.bfloat16, device=dev)
         qo = _packed(q_out, (n, hq, dim), torch.bfloat16, dev, "q_out")
         o = _qk_opts(dim, dev, inv_freq, q_weight, k_weight, eps, interleaved, mscale)
-        _check(lib().sq_qkv_store(self._handle, _i32(layer, "layer"), qp, qs, kp, ks, vp, vs,
+        _check(lib().sq_qkv_store(self._handle, _i32(index(layer), "layer"), qp, qs, kp, ks, vp, vs,
                                   None if o is None else C.byref(o), qo, _stream(stream)))
         return q_out
 
@@ -697,7 +698,7 @@ class Store:
         if not -(1 << 63) <= length < 1 << 63:
             raise SqError(ERR_INVALID, f"length {length} is no 64-bit integer")
         st = C.c_void_p(0) if self.metadata_only else _stream(stream)
-        _check(lib().sq_truncate(self._handle, _i32(seq, "sequence"), length, st))
+        _check(lib().sq_truncate(self._handle, _i32(index(seq), "sequence"), length, st))
 
     # -- drafted tokens ------------------------------------------------------------
     def draft_begin(self, seqs, parents, window=0, first=0, stream=None):
@@ -736,7 +737,7 @@ class Store:
             scale = 1.0 / float(self.head_dim) ** 0.5
         qp, op = self._qo_ptrs(q, out, n)
         o = self._opts(window, sinks, first if window else 0)
-        _check(lib().sq_draft_attn(self._handle, _i32(layer, "layer"), qp, op, float(scale),
+        _check(lib().sq_draft_attn(self._handle, _i32(index(layer), "layer"), qp, op, float(scale),
                                    None if o is None else C.byref(o), _stream(stream)))
         return out
 

@@ -57,6 +57,15 @@ def test_lengths_counts_and_handles(sq, store):
     assert s.positions(h).tolist() == list(range(9))
 
 
+def test_handles_and_layers_are_whole(sq, store):
+    """As ctypes has it for every other call: no number is cut to an integer."""
+    s, h = store
+    for handle in (h + 0.5, "0", None):
+        with pytest.raises(TypeError):
+            s.truncate(handle, 3)
+    assert s.seq_info(h)["length"] == 9
+
+
 def test_integers_that_fit_stay_as_they_were(sq, store):
     import numpy as np
     s, h = store
